@@ -222,6 +222,92 @@ mixaq_status mixaq_embed_forward(mixaq_ctx* ctx, const mixaq_embed_params* p, co
 mixaq_status mixaq_norm_forward(mixaq_ctx* ctx, const float* gamma, const float* beta, const float* x, float* y,
                                 long rows, int C, void* cuda_stream);
 
+/* ---- row operators: 8-bit floating-point codes with block scales, their product, and the norms at a sublayer's border.
+ *      They work on row-major matrices of any size; a row stride is a number of elements, strides and row counts are 64-bit.
+ *      The context's device has to be the current one.  A call with no rows returns MIXAQ_OK without a launch.  Calls use no memory
+ *      beyond their arguments, may be captured, and what lies behind a matrix's last row or last column is neither read nor written. ---- */
+typedef enum { MIXAQ_F32 = 0, MIXAQ_BF16 = 1, MIXAQ_F16 = 2 } mixaq_dtype;
+
+/* A matrix of e4m3 codes (4 exponent bits, bias 7, 3 mantissa bits, no infinities, largest value 448) with one binary32 scale for each
+ * block of `block_rows` rows (1 or 128) by 128 columns, counted from the matrix's corner; blocks at the edges are smaller.
+ *   value(r, c) = codes[r*row_stride + c] * scale[(r/block_rows)*scale_row_stride + (c/128)*scale_col_stride]
+ * codes are 16-byte aligned and row_stride is a multiple of 16 and at least cols (the TMA unit reads them); scales are 4-byte aligned
+ * and lie in any order (for single rows scale_row_stride = 1 is fastest); as an output, no two may share a place.  rows and cols are
+ * below 2^31 - 256, row_stride below 2^40. */
+typedef struct {
+  uint8_t* codes; int64_t rows, cols, row_stride;
+  int block_rows;
+  float* scale; int64_t scale_row_stride, scale_col_stride;
+} mixaq_fp8_matrix;
+
+/* Quantizes x [rows][cols] into `out` (out->rows, cols: those of x, with transpose != 0 exchanged, and the blocks are those of the
+ * transposed matrix: what the gradient products need).  Per block: amax = max |x|;
+ *   scale = max(amax / 448, 2^-126), or with pow2 != 0 the smallest power of two from 2^-126 on that is not below amax / 448;
+ *   code  = e4m3(x * (1 / scale)), to nearest even, at most +-448 (binary32 quotients and product).
+ * A block that holds an infinity or no number gets the scale NaN and NaN codes, so that it shows in every product it enters.
+ * x needs the alignment of its elements only; 16-byte aligned rows read fastest. */
+mixaq_status mixaq_fp8_quantize(mixaq_ctx* ctx, const void* x, mixaq_dtype dtype, int64_t rows, int64_t cols, int64_t row_stride,
+                                int transpose, int pow2, const mixaq_fp8_matrix* out, void* cuda_stream);
+
+/* y [a->rows][w->rows] = a w^T + bias:  y(m, n) = sum_c a(m, c) w(n, c) + bias[n], rounded once to `y_dtype`.
+ * The products of the 128 codes of a block are summed by the tensor cores in binary32, the blocks' sums scaled and added in binary32
+ * in ascending order (few output tiles: in up to 8 parts of ascending blocks, added in order), so results do not depend on anything
+ * but the arguments.  a->cols == w->cols >= 1.  bias: binary32, nullable.  y needs the alignment of its elements only. */
+mixaq_status mixaq_fp8_matmul(mixaq_ctx* ctx, const mixaq_fp8_matrix* a, const mixaq_fp8_matrix* w, const float* bias,
+                              void* y, mixaq_dtype y_dtype, int64_t y_row_stride, void* cuda_stream);
+
+/* The border between two sublayers:
+ *   x_out = x + scale * gate o norm_post(y)          (rounded to x_dtype)
+ *   h     = norm_pre(x_out)                          (of the rounded x_out: the same as two calls)
+ * x, x_out: the residual stream; y: what a sublayer returned; h: the input of the next one, in y_dtype or as e4m3 codes.
+ *   norm MIXAQ_NORM_NONE: v;  MIXAQ_NORM_LAYER: gamma (v - mean) / sqrt(var + eps) + beta;  MIXAQ_NORM_RMS: gamma v / sqrt(mean(v^2) + eps) + beta
+ * gamma and beta are binary32 [dim]; NULL stands for ones and zeros.  eps > 0.
+ * The gate of row r is row r / rows_per_gate of `gate`: rows_per_gate >= rows is a gate per channel, the length of a sequence a gate
+ * per sequence, 1 a gate per token; gate == NULL: ones.
+ * y == NULL: x_out = x, only h is computed (gate and post do not count).  h_fp8 != NULL: h is quantized as by mixaq_fp8_quantize
+ * into this matrix (block_rows 1) and `h` is not used.  pre.kind NONE: no h (h and h_fp8 NULL).
+ * x_out may be x, and h may be y (same address and stride); no other outputs may overlap.  1 <= dim <= MIXAQ_NORM_MAX_DIM.
+ * Pointers need the alignment of their elements; 16-byte aligned rows and a dim that is a multiple of 8 run fastest.
+ * Type pairs (x, y): (F32, any), (BF16, BF16), (F16, F16).  gate_dtype: y_dtype or MIXAQ_F32. */
+#define MIXAQ_NORM_MAX_DIM 16384
+typedef enum { MIXAQ_NORM_NONE = 0, MIXAQ_NORM_LAYER = 1, MIXAQ_NORM_RMS = 2 } mixaq_norm_kind;
+typedef struct { mixaq_norm_kind kind; const float *gamma, *beta; float eps; } mixaq_norm;
+typedef struct {
+  int64_t rows; int dim;
+  mixaq_dtype x_dtype, y_dtype, gate_dtype;
+  const void* x; int64_t x_stride;
+  const void* y; int64_t y_stride;                   /* nullable */
+  const void* gate; int64_t gate_stride, rows_per_gate;    /* nullable */
+  float scale;
+  mixaq_norm post, pre;
+  void* x_out; int64_t x_out_stride;                 /* with y only */
+  void* h; int64_t h_stride;
+  const mixaq_fp8_matrix* h_fp8; int pow2;
+} mixaq_residual_norm_params;
+mixaq_status mixaq_residual_norm_forward(mixaq_ctx* ctx, const mixaq_residual_norm_params* p, void* cuda_stream);
+
+/* Its gradients.  Of `p` are read: rows, dim, the types, x and x_stride, which are here the x_out that the forward call WROTE (its
+ * x without y), y, gate, scale, post and pre.  dx_out and dh: gradients of x_out (x_dtype) and of h (y_dtype); one of the two may be
+ * NULL (dx_out: nothing but h was used; dh: there is no pre norm).  Quantizing h counts as the identity.
+ *   dx     = dx_out + J_pre^T dh                    rounded to x_dtype; the rest is computed from the unrounded sum
+ *   dgate  = sum over the gate's rows of scale * dx o norm_post(y)              binary32 [gates][dim]
+ *   dy     = J_post^T (scale * gate o dx)           y_dtype
+ *   d*_gamma, d*_beta                               binary32 [dim], sums over the rows
+ * Every output may be NULL.  dx may be dx_out, dy may be dh or y (same address and stride).  Sums over rows are added in an order that
+ * depends on the sizes and the device only.  workspace: 256-byte aligned; not shared by calls that can overlap.
+ * rows == 0 writes zeros to dgate's rows (none) and to the parameter gradients. */
+typedef struct {
+  const void* dx_out; int64_t dx_out_stride;
+  const void* dh; int64_t dh_stride;
+  void* dx; int64_t dx_stride;
+  void* dy; int64_t dy_stride;
+  float* dgate; int64_t dgate_stride;
+  float *dpost_gamma, *dpost_beta, *dpre_gamma, *dpre_beta;
+} mixaq_residual_norm_grads;
+size_t       mixaq_residual_norm_backward_workspace_bytes(const mixaq_residual_norm_params* p);
+mixaq_status mixaq_residual_norm_backward(mixaq_ctx* ctx, const mixaq_residual_norm_params* p, const mixaq_residual_norm_grads* g,
+                                          void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* ---- calibration of the activation quantizers (Section 4.3, post-training flow): one calibration sample, and the
  *      FULL feature map (every window, whatever branch it will later run in) sets the ranges of BOTH branches, which
  *      then differ only in bit width.  mixaq_calibrate_block runs the floating-point block (all quantizers off,

@@ -25,6 +25,7 @@ EXPORTS = [
     "mixaq_embed_prepared_bytes", "mixaq_embed_prepare", "mixaq_embed_workspace_bytes", "mixaq_embed_forward",
     "mixaq_norm_forward", "mixaq_profile_end_records", "mixaq_calibrate_block_workspace_bytes", "mixaq_calibrate_block",
     "mixaq_calibrate_merge_workspace_bytes", "mixaq_calibrate_merge", "mixaq_aq_from_range", "mixaq_clear_device_status", "mixaq_selftest_wait_timeout", "mixaq_measure_mma_peak", "mixaq_set_window_elevation", "mixaq_set_reverse_selection", "mixaq_set_nvtx", "mixaq_set_workspace_guards", "mixaq_selftest_workspace_guards",
+    "mixaq_fp8_quantize", "mixaq_fp8_matmul",
 ]
 
 STATUS = {0: "OK", -1: "INVALID_ARG", -2: "UNSUPPORTED_SHAPE", -3: "WORKSPACE_TOO_SMALL", -4: "CUDA_ERROR",
@@ -549,3 +550,111 @@ def backbone_forward(ctx: Context, dbb: DeviceBackbone, x0: torch.Tensor, low_ra
                                       _ptr(dbb.ws), C.c_size_t(dbb.ws.numel()), _stream_ptr())
     ctx.check(st, "backbone_forward")
     return dbb.outs
+
+
+# ---- row operators: e4m3 codes with block scales, their product, the norms at a sublayer's border ---------------------------------
+FP8_BLOCK = 128
+NORM_MAX_DIM = 16384
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_NORM_KINDS = {"layer": 1, "rms": 2}
+
+
+class Fp8MatrixS(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("row_stride", C.c_int64), ("block_rows", C.c_int),
+                ("scale", C.c_void_p), ("scale_row_stride", C.c_int64), ("scale_col_stride", C.c_int64)]
+
+
+def _need(ok, what: str):
+    if not ok:
+        raise MixaqError(-1, what)
+
+
+def _matrix(ctx: Context, t: torch.Tensor, name: str, dtypes=_DTYPES):
+    """Checks a 2-D tensor whose rows are contiguous; returns its row stride (that of a single row counts as its length)."""
+    _need(isinstance(t, torch.Tensor) and t.dim() == 2, f"{name}: a 2-D tensor is needed")
+    _need(t.device == ctx.device, f"{name}: on {t.device}, the context's device is {ctx.device}")
+    _need(t.dtype in dtypes, f"{name}: unsupported dtype {t.dtype}")
+    rows, cols = t.shape
+    _need(cols <= 1 or t.stride(1) == 1, f"{name}: the elements of a row must be neighbours")
+    return t.stride(0) if rows > 1 else max(t.stride(0), cols)
+
+
+def _vector(ctx: Context, t: Optional[torch.Tensor], n: int, name: str):
+    if t is None:
+        return None
+    _need(t.device == ctx.device and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == (n,),
+          f"{name}: a contiguous float32 vector of {n} on {ctx.device} is needed")
+    return _ptr(t)
+
+
+class Fp8Matrix:
+    """A matrix of e4m3 codes with a scale per block of block_rows x 128 (mixaq_fp8_matrix).
+    codes: [rows, cols] float8_e4m3fn, 16-byte aligned, row stride a multiple of 16; scale: [ceil(rows/block_rows), ceil(cols/128)]
+    float32 in any order."""
+
+    def __init__(self, codes: torch.Tensor, scale: torch.Tensor, block_rows: int = 1):
+        self.codes, self.scale, self.block_rows = codes, scale, block_rows
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, block_rows: int, device) -> "Fp8Matrix":
+        """Room for a matrix: rows padded to a multiple of 16 bytes; scales of single rows with the rows as neighbours."""
+        ld = -(-cols // 16) * 16
+        codes = torch.empty((rows, ld), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+        rb, cb = -(-rows // block_rows), -(-cols // FP8_BLOCK)
+        scale = torch.empty((cb, rb), dtype=torch.float32, device=device).t() if block_rows == 1 else \
+            torch.empty((rb, cb), dtype=torch.float32, device=device)
+        return cls(codes, scale, block_rows)
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    def struct(self, ctx: Context, name: str) -> Fp8MatrixS:
+        rows, cols = self.codes.shape if self.codes.dim() == 2 else (0, 0)
+        ld = _matrix(ctx, self.codes, name + ".codes", (torch.float8_e4m3fn,))
+        if rows <= 1:
+            ld = -(-ld // 16) * 16            # (a single row has no stride)
+        _need(self.block_rows in (1, FP8_BLOCK), f"{name}: block_rows must be 1 or {FP8_BLOCK}")
+        want = (-(-rows // self.block_rows), -(-cols // FP8_BLOCK))
+        s = self.scale
+        _need(isinstance(s, torch.Tensor) and s.device == ctx.device and s.dtype == torch.float32 and tuple(s.shape) == want,
+              f"{name}.scale: a float32 tensor {want} on {ctx.device} is needed")
+        return Fp8MatrixS(self.codes.data_ptr(), rows, cols, ld, self.block_rows, s.data_ptr(), s.stride(0), s.stride(1))
+
+    def values(self) -> torch.Tensor:
+        """The float32 values that the codes stand for (a plain torch expression, for inspection)."""
+        rows, cols = self.codes.shape
+        s = self.scale.repeat_interleave(self.block_rows, dim=0)[:rows].repeat_interleave(FP8_BLOCK, dim=1)[:, :cols]
+        return self.codes.float() * s
+
+
+def fp8_quantize(ctx: Context, x: torch.Tensor, block_rows: int = 1, transpose: bool = False, pow2: bool = False,
+                 out: Optional[Fp8Matrix] = None) -> Fp8Matrix:
+    """mixaq_fp8_quantize: x [rows, cols] (float32, bfloat16, float16) to e4m3 codes with a scale per block of block_rows (1 or 128)
+    by 128 columns; transpose: of the transposed matrix; pow2: scales that are powers of two."""
+    ld = _matrix(ctx, x, "x")
+    rows, cols = x.shape
+    _need(block_rows in (1, FP8_BLOCK), f"block_rows must be 1 or {FP8_BLOCK}")
+    r, c = (cols, rows) if transpose else (rows, cols)
+    if out is None:
+        out = Fp8Matrix.empty(r, c, block_rows, x.device)
+    _need(out.block_rows == block_rows, "out has other blocks")
+    s = out.struct(ctx, "out")
+    ctx.check(lib().mixaq_fp8_quantize(ctx.h, _ptr(x), _DTYPES[x.dtype], C.c_int64(rows), C.c_int64(cols), C.c_int64(ld),
+                                       1 if transpose else 0, 1 if pow2 else 0, C.byref(s), _stream_ptr()), "fp8_quantize")
+    return out
+
+
+def fp8_matmul(ctx: Context, a: Fp8Matrix, w: Fp8Matrix, bias: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
+               y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """mixaq_fp8_matmul: y [a.rows, w.rows] = a w^T + bias in out_dtype (float32, bfloat16, float16)."""
+    sa, sw = a.struct(ctx, "a"), w.struct(ctx, "w")
+    m, n = sa.rows, sw.rows
+    if y is None:
+        _need(out_dtype in _DTYPES, f"unsupported out_dtype {out_dtype}")
+        y = torch.empty((m, n), dtype=out_dtype, device=a.codes.device)
+    ld = _matrix(ctx, y, "y")
+    _need(tuple(y.shape) == (m, n), f"y: {(m, n)} is needed")
+    ctx.check(lib().mixaq_fp8_matmul(ctx.h, C.byref(sa), C.byref(sw), _vector(ctx, bias, n, "bias"), _ptr(y), _DTYPES[y.dtype],
+                                     C.c_int64(ld), _stream_ptr()), "fp8_matmul")
+    return y

@@ -3,8 +3,11 @@ the product is a plain C-ABI shared object declared in include/mixaq.h."""
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -33,10 +36,21 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + sources() + ["-lcuda", "-ldl"]
-    # libcuda is only needed for the tensor-map encoder; resolve it lazily so the build works without a driver
-    cmd = [c for c in cmd if c != "-lcuda"]
-    subprocess.check_call(cmd)
+    flags = NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else [])
+    # the sources are compiled side by side; libcuda is only needed for the tensor-map encoder, which is resolved lazily, so that
+    # the build works without a driver
+    with tempfile.TemporaryDirectory() as tmp:
+        def compile_one(source):
+            obj = os.path.join(tmp, os.path.basename(source) + ".o")
+            subprocess.check_call([nvcc] + [f for f in flags if f != "-shared"] + ["-c", "-o", obj, source])
+            return obj
+        with ThreadPoolExecutor(os.cpu_count() or 1) as pool:
+            objects = list(pool.map(compile_one, sources()))
+        out = os.path.join(tmp, "libmixaq.so")
+        subprocess.check_call([nvcc] + NVCC_FLAGS + ["-o", out] + objects + ["-ldl"])
+        new = f"{LIB[:-3]}.{os.getpid()}.so"             # in place at once: another process may be loading the library
+        shutil.copyfile(out, new)
+        os.replace(new, LIB)
     return LIB
 
 

@@ -1,0 +1,490 @@
+// Product of two e4m3 matrices with block scales (mixaq_fp8_matmul) on the 5th-generation tensor cores (tcgen05.mma kind::f8f6f4).
+//
+//   y(m, n) = sum_b sa(m, b) sw(n, b) d_b(m, n) + bias(n),   d_b(m, n) = sum of the 128 products of k-block b
+//
+// The scales change from k-block to k-block, so the tensor memory holds one k-block's sums d_b at a time and the epilogue warps keep the
+// running sums in registers: per k-block they read d_b (tcgen05.ld) and add scale * d_b with packed fused multiply-adds, while the tensor
+// core fills the next accumulator.  A k-block of a 128 x BN tile takes the tensor core BN cycles (8 192 multiply-adds a cycle and SM) and
+// the FMA pipe BN / 2 (128 packed lanes a cycle): the sums fit beneath the MMAs.
+//
+// One CTA per SM walks over 128 x BN output tiles: warp 0 feeds a ring of 128-byte-swizzled stages by TMA (no multicast), warp 1 issues
+// the MMAs, warp 2 brings a k-block's column scales to shared memory where weights have a scale per row, warps 4-11 are the epilogue
+// (warp w has rows 32 (w % 4) ... of the tile and half of its columns).  Where there are few tiles, a cluster of up to 8 CTAs divides
+// the k-blocks of a tile and adds its parts through distributed shared memory, in the order of the ranks.
+// Every wait on an mbarrier is bounded, as in gemm_tc.cu.
+#include "kernels.h"
+#include "fp8.cuh"
+#include "tc_ptx.cuh"
+#include <atomic>
+#include <cstring>
+
+namespace mixaq {
+namespace {
+
+constexpr int BM = 128, BK = 128, UMMA_K = 32;
+constexpr int A_BYTES = BM * BK;
+constexpr int EPI_WARPS = 8, FIRST_EPI = 4, THREADS = 32 * (FIRST_EPI + EPI_WARPS);
+constexpr int STAGING = 2048;                  // bytes of an epilogue warp's store buffer: 32 rows of 64
+constexpr int MAX_SPLIT = 8;
+constexpr int MAX_ACC = 4, MAX_RING = 8;
+__host__ __device__ constexpr int num_acc(int bn) { return bn == 256 ? 2 : MAX_ACC; }
+__host__ __device__ constexpr int ring_stages(int bn) { return bn == 256 ? 4 : bn == 128 ? 6 : MAX_RING; }
+__host__ __device__ constexpr int tmem_cols(int bn) { return num_acc(bn) * bn; }
+__host__ __device__ constexpr int stage_bytes(int bn) { return A_BYTES + bn * BK; }
+// Wide tiles keep 128 sums a thread: the side warpgroup gives up registers for them (4 x 72 + 8 x 216 of 12 x 168).
+constexpr int SIDE_REGS = 72, EPI_REGS = 216;
+__host__ __device__ constexpr bool exchanges_registers(int bn) { return bn == 256; }
+constexpr int NUM_BARS = 2 * MAX_RING + 3 * MAX_ACC + 1;        // stage full, empty; accumulator full, empty, column scales; drain
+
+__host__ __device__ constexpr int smem_total(int bn) {
+  return ring_stages(bn) * stage_bytes(bn) + EPI_WARPS * STAGING + num_acc(bn) * bn * 4 + NUM_BARS * 8 + 16;
+}
+
+struct Params {
+  Fp8MatmulArgs g;
+  int M, N, k_blocks;
+  int m_tiles, n_tiles, tiles, split;          // split: CTAs of a cluster that share a tile (1: no cluster)
+};
+
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// 16 columns of the warp's 32 rows, one row per thread; valid after tmem_wait16
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+        "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+      : "r"(taddr) : "memory");
+}
+// waits for all loads; the registers pass through so that no use of them is scheduled ahead of it
+__device__ __forceinline__ void tmem_wait16(float* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+      : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),
+        "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]) :: "memory");
+}
+__device__ __forceinline__ void pass_through16(float* r) {
+  asm volatile("" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),
+        "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]));
+}
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ float4 ld_cluster(uint32_t addr, uint32_t rank) {
+  uint32_t a;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+  return v;
+}
+
+// n (<= E) elements of a row to memory, as one piece where all are there and the address allows it
+template <class T, int E>
+__device__ __forceinline__ void store_piece(T* p, const T (&v)[E], bool vec, int n) {
+  if (vec && n >= E) {
+    if constexpr (sizeof(T) * E == 16) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(v);
+    else *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) if (i < n) p[i] = v[i];
+  }
+}
+
+// The warp's 32 rows x COLS columns, through its staging buffer: rows of P 16-byte pieces, piece p of row r at p ^ (r / 2), so that
+// eight lanes with a row each and four lanes a row both spread over all banks; memory is written in 64-byte runs.
+template <class T, int COLS>
+__device__ __forceinline__ void store_tile(const float2 (&acc)[COLS / 2], uint8_t* staging, const Params& p, int row0, int col0, int lane) {
+  constexpr int E = 16 / (int)sizeof(T), P = COLS / E < 4 ? COLS / E : 4, CHUNK = P * E, PER = 32 / P;
+  T* const y = static_cast<T*>(p.g.y);
+  const bool vec = reinterpret_cast<uintptr_t>(y) % 16 == 0 && p.g.y_stride * (long)sizeof(T) % 16 == 0;
+  const float* bias = p.g.bias;
+#pragma unroll
+  for (int ch = 0; ch < COLS / CHUNK; ++ch) {
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+      T v[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const int c = ch * CHUNK + q * E + i;
+        float f = c & 1 ? acc[c / 2].y : acc[c / 2].x;
+        if (bias) f = __fadd_rn(f, __ldg(bias + min(col0 + c, p.N - 1)));
+        v[i] = from_f32<T>(f);
+      }
+      *reinterpret_cast<uint4*>(staging + lane * 64 + ((q ^ (lane >> 1)) & (P - 1)) * 16) = *reinterpret_cast<const uint4*>(v);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int r = i * PER + lane / P, q = lane % P, col = col0 + ch * CHUNK + q * E;
+      const uint4 w = *reinterpret_cast<const uint4*>(staging + r * 64 + ((q ^ (r >> 1)) & (P - 1)) * 16);
+      T v[E];
+      *reinterpret_cast<uint4*>(v) = w;
+      if (row0 + r < p.M) store_piece<T, E>(y + (long)(row0 + r) * p.g.y_stride + col, v, vec, p.N - col);
+    }
+    __syncwarp();
+  }
+}
+
+// Sum of the cluster's parts of a tile, 128 x BN binary32 in every CTA's shared memory at `part` (four-column piece q of row r at
+// q ^ (r % 8)); this CTA adds and stores its share of the rows.
+template <class T, int BN>
+__device__ __forceinline__ void join_parts(uint32_t part, const Params& p, int rank, int m0, int n0, int tid) {
+  T* const y = static_cast<T*>(p.g.y);
+  const bool vec = reinterpret_cast<uintptr_t>(y) % 16 == 0 && p.g.y_stride * (long)sizeof(T) % 16 == 0;
+  const int rows = BM / p.split;
+  const float* bias = p.g.bias;
+  for (int i = tid; i < rows * (BN / 4); i += EPI_WARPS * 32) {
+    const int r = rank * rows + i / (BN / 4), q = i % (BN / 4), col = n0 + q * 4;
+    if (m0 + r >= p.M || col >= p.N) continue;
+    const uint32_t at = part + (uint32_t)((r * (BN / 4) + (q ^ (r & 7))) * 16);
+    float4 s = ld_cluster(at, 0);
+    for (int j = 1; j < p.split; ++j) {
+      const float4 v = ld_cluster(at, j);
+      s.x = __fadd_rn(s.x, v.x); s.y = __fadd_rn(s.y, v.y); s.z = __fadd_rn(s.z, v.z); s.w = __fadd_rn(s.w, v.w);
+    }
+    float f[4] = {s.x, s.y, s.z, s.w};
+    T v[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      if (bias) f[c] = __fadd_rn(f[c], __ldg(bias + min(col + c, p.N - 1)));
+      v[c] = from_f32<T>(f[c]);
+    }
+    store_piece<T, 4>(y + (long)(m0 + r) * p.g.y_stride + col, v, vec, p.N - col);
+  }
+}
+
+struct Ring {
+  int slot = 0; uint32_t pass = 0;
+  __device__ __forceinline__ void next(int n) { if (++slot == n) { slot = 0; pass ^= 1u; } }
+};
+
+// Tiles are walked in bands of 8 row tiles, so that the CTAs at work share rows of both operands in the L2.
+constexpr int BAND = 8;
+__device__ __forceinline__ void tile_at(const Params& p, int t, int& mt, int& nt) {
+  const int per = BAND * p.n_tiles, band = t / per, in = t - band * per;
+  const int height = min(BAND, p.m_tiles - band * BAND);
+  nt = in / height;
+  mt = band * BAND + in - nt * height;
+}
+
+// COLSCALE: the weights have a scale per row, so every column of a tile has one of its own
+template <int BN, bool COLSCALE>
+__global__ void __launch_bounds__(THREADS, 1)
+k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ Params p) {
+  constexpr int N_ACC = num_acc(BN), RING = ring_stages(BN), STAGE = stage_bytes(BN), COLS = BN / 2;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;     // swizzled tiles need 1024-byte alignment
+  uint8_t* const smem = smem_raw + (base - raw);
+  uint8_t* const staging = smem + RING * STAGE;
+  float* const col_scales = reinterpret_cast<float*>(staging + EPI_WARPS * STAGING);      // [N_ACC][BN]
+  uint64_t* const bars = reinterpret_cast<uint64_t*>(col_scales + N_ACC * BN);
+  const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8u * MAX_RING, bar_tfull = bar_empty + 8u * MAX_RING;
+  const uint32_t bar_tempty = bar_tfull + 8u * MAX_ACC, bar_cols = bar_tempty + 8u * MAX_ACC, bar_drain = bar_cols + 8u * MAX_ACC;
+  uint32_t* const tmem_holder = reinterpret_cast<uint32_t*>(bars + NUM_BARS);
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  uint32_t fills = 0;                          // TMA warp: fills of ring stages so far
+
+  if (tid == 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmA) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmW) : "memory");
+  }
+  if (tid == 0) {
+    for (int s = 0; s < RING; ++s) { mbar_init(bar_full + 8u * s, 1u); mbar_init(bar_empty + 8u * s, 1u); }
+    for (int a = 0; a < N_ACC; ++a) {
+      mbar_init(bar_tfull + 8u * a, 1u); mbar_init(bar_tempty + 8u * a, EPI_WARPS); mbar_init(bar_cols + 8u * a, 1u);
+    }
+    mbar_init(bar_drain, 1u);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32(tmem_holder)), "r"((uint32_t)tmem_cols(BN)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_base = *tmem_holder;
+  griddep_wait();                              // operands, scales and y may belong to earlier kernels
+  griddep_launch();
+  if (exchanges_registers(BN) && warp < FIRST_EPI) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(SIDE_REGS));
+
+  // this CTA's tiles and, in a cluster, its share of the k-blocks
+  const int rank = p.split > 1 ? (int)(blockIdx.x % (unsigned)p.split) : 0;
+  const int first = (int)(blockIdx.x / (unsigned)p.split), step = (int)(gridDim.x / (unsigned)p.split);
+  const int kb0 = (int)((long)p.k_blocks * rank / p.split), kb1 = (int)((long)p.k_blocks * (rank + 1) / p.split);
+
+  if (warp == 0) {
+    const bool leader = elect_one();
+    Ring rp;
+    bool ok = true;
+    for (int t = first; t < p.tiles && ok; t += step) {
+      int mt, nt;
+      tile_at(p, t, mt, nt);
+      for (int kb = kb0; kb < kb1; ++kb, rp.next(RING)) {
+        const uint32_t o = 8u * (uint32_t)rp.slot, sa = base + (uint32_t)(rp.slot * STAGE);
+        if (!mbar_wait_warp(bar_empty + o, rp.pass ^ 1u, abort_flag)) { ok = false; break; }
+        ++fills;
+        if (leader) {
+          mbar_arrive_expect_tx(bar_full + o, (uint32_t)STAGE);
+          tma_load_2d(sa, &tmA, kb * BK, mt * BM, bar_full + o);
+          tma_load_2d(sa + A_BYTES, &tmW, kb * BK, nt * BN, bar_full + o);
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp == 1) {
+    const bool leader = elect_one();
+    // D binary32 (1 at bit 4), A and B e4m3 (0 at bits 7 and 10), N / 8, M / 16
+    const uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+    const uint64_t adesc0 = smem_desc_sw128(base), bdesc0 = smem_desc_sw128(base + A_BYTES);
+    Ring rp, ap;
+    bool ok = true;
+    for (int t = first; t < p.tiles && ok; t += step) {
+      for (int kb = kb0; kb < kb1; ++kb, rp.next(RING), ap.next(N_ACC)) {
+        const uint32_t o = 8u * (uint32_t)rp.slot;
+        if (!mbar_wait_warp<true>(bar_tempty + 8u * ap.slot, ap.pass ^ 1u, abort_flag)) { ok = false; break; }
+        if (!mbar_wait_warp<true>(bar_full + o, rp.pass, abort_flag)) { ok = false; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint64_t so = (uint64_t)((uint32_t)(rp.slot * STAGE) >> 4);
+        const uint32_t d = tmem_base + (uint32_t)(ap.slot * BN);
+        if (leader) {
+#pragma unroll
+          for (int kk = 0; kk < BK / UMMA_K; ++kk)
+            mma_f8(d, adesc0 + so + (uint64_t)(kk * (UMMA_K >> 4)), bdesc0 + so + (uint64_t)(kk * (UMMA_K >> 4)), idesc, kk > 0 ? 1u : 0u);
+          mma_commit(bar_empty + o);
+          mma_commit(bar_tfull + 8u * ap.slot);
+        }
+        __syncwarp();
+      }
+    }
+  } else if (COLSCALE && warp == 2) {
+    // column scales of a k-block, for the accumulator of the same number; loaded one k-block ahead
+    Ring ap;
+    bool ok = true;
+    for (int t = first; t < p.tiles && ok; t += step) {
+      int mt, nt;
+      tile_at(p, t, mt, nt);
+      float v[BN / 32];
+      auto load = [&](int kb) {
+#pragma unroll
+        for (int i = 0; i < BN / 32; ++i) v[i] = __ldg(p.g.w.scale + (long)min(nt * BN + i * 32 + lane, p.N - 1) * p.g.w.srs + (long)kb * p.g.w.scs);
+      };
+      load(kb0);
+      for (int kb = kb0; kb < kb1; ++kb, ap.next(N_ACC)) {
+        if (!mbar_wait_warp(bar_tempty + 8u * ap.slot, ap.pass ^ 1u, abort_flag)) { ok = false; break; }
+#pragma unroll
+        for (int i = 0; i < BN / 32; ++i) col_scales[ap.slot * BN + i * 32 + lane] = v[i];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_cols + 8u * ap.slot);
+        if (kb + 1 < kb1) load(kb + 1);
+      }
+    }
+  } else if (warp >= FIRST_EPI) {
+    if (exchanges_registers(BN)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(EPI_REGS));
+    const int q = warp & 3, half = (warp - FIRST_EPI) >> 2;
+    const uint32_t tmem_q = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * COLS);
+    uint8_t* const my_staging = staging + (warp - FIRST_EPI) * STAGING;
+    Ring ap;
+    bool ok = true;
+    for (int t = first; t < p.tiles && ok; t += step) {
+      int mt, nt;
+      tile_at(p, t, mt, nt);
+      const int row0 = mt * BM + q * 32, col0 = nt * BN + half * COLS;
+      const float* const sa = p.g.a.scale + (long)(min(row0 + lane, p.M - 1) / p.g.a.block_rows) * p.g.a.srs;
+      const float* const sw = p.g.w.scale + (COLSCALE ? 0L : (long)(min(col0, p.N - 1) / p.g.w.block_rows) * p.g.w.srs);
+      auto scale_of = [&](int kb) {
+        const float s = __ldg(sa + (long)kb * p.g.a.scs);
+        return COLSCALE ? s : __fmul_rn(s, __ldg(sw + (long)kb * p.g.w.scs));
+      };
+      float2 acc[COLS / 2];
+#pragma unroll
+      for (int i = 0; i < COLS / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
+      // scales two k-blocks ahead
+      float s1 = scale_of(kb0), s2 = kb0 + 1 < kb1 ? scale_of(kb0 + 1) : 0.0f;
+      for (int kb = kb0; kb < kb1; ++kb, ap.next(N_ACC)) {
+        const float2 s = f2(s1);
+        s1 = s2;
+        if (kb + 2 < kb1) s2 = scale_of(kb + 2);
+        if (COLSCALE && !mbar_wait_warp<true>(bar_cols + 8u * ap.slot, ap.pass, abort_flag)) { ok = false; break; }
+        if (!mbar_wait_warp<true>(bar_tfull + 8u * ap.slot, ap.pass, abort_flag)) { ok = false; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        constexpr int LD = COLS < 64 ? COLS : 64;             // columns in flight
+        const uint32_t d = tmem_q + (uint32_t)(ap.slot * BN);
+        const float4* const cs = reinterpret_cast<const float4*>(col_scales + ap.slot * BN + half * COLS);
+#pragma unroll
+        for (int c = 0; c < COLS; c += LD) {
+          float r[LD];
+#pragma unroll
+          for (int i = 0; i < LD; i += 16) tmem_ld16(d + (uint32_t)(c + i), r + i);
+          tmem_wait16(r);
+#pragma unroll
+          for (int i = 16; i < LD; i += 16) pass_through16(r + i);
+          if (!COLSCALE && c + LD == COLS) {                  // all is read: the tensor core may have the accumulator back
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_tempty + 8u * ap.slot);
+          }
+#pragma unroll
+          for (int i = 0; i < LD; i += 4) {
+            float2 d0 = make_float2(r[i], r[i + 1]), d1 = make_float2(r[i + 2], r[i + 3]);
+            if (COLSCALE) {
+              const float4 w = cs[(c + i) / 4];
+              d0 = __fmul2_rn(d0, make_float2(w.x, w.y)); d1 = __fmul2_rn(d1, make_float2(w.z, w.w));
+            }
+            acc[(c + i) / 2] = __ffma2_rn(d0, s, acc[(c + i) / 2]);
+            acc[(c + i) / 2 + 1] = __ffma2_rn(d1, s, acc[(c + i) / 2 + 1]);
+          }
+        }
+        if (COLSCALE) {                                       // (the scales beside it have been read, too)
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_tempty + 8u * ap.slot);
+        }
+      }
+      if (!ok) break;
+      if (p.split == 1) {
+        if (p.g.y_dtype == DT_F32) store_tile<float, COLS>(acc, my_staging, p, row0, col0, lane);
+        else if (p.g.y_dtype == DT_BF16) store_tile<__nv_bfloat16, COLS>(acc, my_staging, p, row0, col0, lane);
+        else store_tile<__half, COLS>(acc, my_staging, p, row0, col0, lane);
+      } else if (BN <= 128) {
+        // the part goes where the ring was: every stage has been multiplied when the last accumulator is complete
+        const int r = q * 32 + lane;
+#pragma unroll
+        for (int i = 0; i < COLS / 4; ++i) {
+          const int piece = half * (COLS / 4) + i;
+          *reinterpret_cast<float4*>(smem + (r * (BN / 4) + (piece ^ (r & 7))) * 16) =
+              make_float4(acc[2 * i].x, acc[2 * i].y, acc[2 * i + 1].x, acc[2 * i + 1].y);
+        }
+      }
+    }
+  }
+
+  __syncwarp();
+  if (p.split > 1) {
+    cluster_sync();
+    if (warp >= FIRST_EPI && BN <= 128 && first < p.tiles) {
+      int mt, nt;
+      tile_at(p, first, mt, nt);
+      const int e = tid - FIRST_EPI * 32;
+      if (p.g.y_dtype == DT_F32) join_parts<float, BN>(base, p, rank, mt * BM, nt * BN, e);
+      else if (p.g.y_dtype == DT_BF16) join_parts<__nv_bfloat16, BN>(base, p, rank, mt * BM, nt * BN, e);
+      else join_parts<__half, BN>(base, p, rank, mt * BM, nt * BN, e);
+    }
+    cluster_sync();                            // nobody leaves while its part is being read
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (*abort_flag) {
+    // A wait ran out: the copies issued must have landed and the MMAs issued must have retired before the CTA may exit (bounded).
+    if (warp == 1 && elect_one()) mma_commit(bar_drain);
+    __syncthreads();
+    if (tid == 0) {
+      atomicExch(p.g.status, 1);
+      auto drain = [](uint32_t bar, uint32_t parity) {
+        for (uint32_t it = 0; it < (1u << 20); ++it) if (mbar_try_wait(bar, parity)) return;
+      };
+      for (uint32_t s = 0; s < (uint32_t)RING; ++s)
+        if (fills > s) drain(bar_full + 8u * s, (fills - 1u - s) / (uint32_t)RING & 1u);
+      drain(bar_drain, 0u);
+    }
+    __syncthreads();
+  }
+  if (warp == 2)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)tmem_cols(BN)) : "memory");
+}
+
+// ---- host side -------------------------------------------------------------------------------------------------------------
+// rows of `cols` bytes, `stride` bytes apart; boxes of box_rows x 128 bytes with 128-byte swizzle, zeros outside
+bool make_rows_map(CUtensorMap* m, const uint8_t* ptr, uint64_t rows, uint64_t cols, uint64_t stride, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {cols, rows}, strides[1] = {stride};
+  cuuint32_t box[2] = {BK, box_rows}, estr[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Plan { int bn, split; };
+Plan pick_plan(long m_tiles, int N, int k_blocks, int sms) {
+  Plan best = {0, 0};
+  double best_cost = 0.0;
+  for (int bn = 32; bn <= 256; bn *= 2) {
+    const long tiles = m_tiles * ((N + bn - 1) / bn);
+    for (int split = 1; split <= MAX_SPLIT; split *= 2) {
+      if (split > 1 && (bn > 128 || split > k_blocks || tiles * split > sms)) break;
+      const long rounds = (tiles * split + sms - 1) / sms;
+      const int blocks = (k_blocks + split - 1) / split;
+      const double block = bn == 256 ? 0.31 : bn == 128 ? 0.17 : 0.13;
+      const double cost = rounds * (blocks * block + (split > 1 ? 1.5 : 0.0) + 0.004 * bn) + 2.0;
+      if (!best.bn || cost <= best_cost) { best = {bn, split}; best_cost = cost; }
+    }
+  }
+  return best;
+}
+
+template <int BN, bool COLSCALE>
+bool set_up() {
+  // per device: opt in to the shared memory, and check that the register shares fit into what the block is launched with
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev > 63) return false;
+  if (done.load(std::memory_order_acquire) >> dev & 1) return true;
+  cudaFuncAttributes at;
+  if (cudaFuncSetAttribute(k_fp8_gemm<BN, COLSCALE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_total(BN) + 1024) != cudaSuccess ||
+      cudaFuncGetAttributes(&at, k_fp8_gemm<BN, COLSCALE>) != cudaSuccess)
+    return false;
+  if (exchanges_registers(BN) && FIRST_EPI * SIDE_REGS + EPI_WARPS * EPI_REGS > (FIRST_EPI + EPI_WARPS) * at.numRegs) return false;
+  done.fetch_or(1ull << dev, std::memory_order_release);
+  return true;
+}
+
+template <int BN, bool COLSCALE>
+bool launch_as(const Params& p, cudaStream_t st, int sms) {
+  static_assert(smem_total(BN) + 1024 <= 227 * 1024, "shared memory");
+  if (!set_up<BN, COLSCALE>()) return false;
+  CUtensorMap mA, mW;
+  if (!make_rows_map(&mA, p.g.a.codes, p.M, p.g.K, p.g.a.stride, BM) || !make_rows_map(&mW, p.g.w.codes, p.N, p.g.K, p.g.w.stride, BN)) return false;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = p.split; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)(p.split > 1 ? p.tiles * p.split : p.tiles < sms ? p.tiles : sms));
+  cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = smem_total(BN) + 1024; cfg.stream = st;
+  cfg.attrs = attr; cfg.numAttrs = p.split > 1 ? 2 : 1;
+  cudaLaunchKernelEx(&cfg, k_fp8_gemm<BN, COLSCALE>, mA, mW, p);
+  ++g_launches;
+  return true;
+}
+
+}  // namespace
+
+bool launch_fp8_matmul(const Fp8MatmulArgs& g, cudaStream_t st) {
+  Params p;
+  p.g = g; p.M = (int)g.a.rows; p.N = (int)g.w.rows;
+  p.k_blocks = (int)((g.K + BK - 1) / BK);
+  p.m_tiles = (p.M + BM - 1) / BM;
+  const int sms = sm_count();
+  const Plan plan = pick_plan(p.m_tiles, p.N, p.k_blocks, sms);
+  p.n_tiles = (p.N + plan.bn - 1) / plan.bn;
+  if ((long)p.m_tiles * p.n_tiles >= (1L << 31) - sms) return false;
+  p.tiles = p.m_tiles * p.n_tiles; p.split = plan.split;
+  const bool cols = g.w.block_rows == 1;
+  switch (plan.bn) {
+    case 32:  return cols ? launch_as<32, true>(p, st, sms) : launch_as<32, false>(p, st, sms);
+    case 64:  return cols ? launch_as<64, true>(p, st, sms) : launch_as<64, false>(p, st, sms);
+    case 128: return cols ? launch_as<128, true>(p, st, sms) : launch_as<128, false>(p, st, sms);
+    case 256: return cols ? launch_as<256, true>(p, st, sms) : launch_as<256, false>(p, st, sms);
+  }
+  return false;
+}
+
+}  // namespace mixaq

@@ -157,6 +157,23 @@ constexpr int CAL_SLICES = 7;                     // byte planes a calibration p
 constexpr int CAL_STATUS = 16, CAL_OBS = 17;      // word of the call's own status behind the 16 keys (the context's may be older)
 float cal_key_to_float(uint32_t key);
 
+// ---- row operators: e4m3 codes with block scales, their product, norms at a sublayer's border ---------------------------------
+enum DType { DT_F32 = 0, DT_BF16 = 1, DT_F16 = 2 };        // values of mixaq_dtype
+struct Fp8QuantArgs {
+  const void* x; int dtype; long rows, cols, row_stride;
+  bool transpose, pow2; int block_rows;
+  uint8_t* codes; long code_stride; float* scale; long scale_row_stride, scale_col_stride;
+};
+void launch_fp8_quantize(const Fp8QuantArgs& a, cudaStream_t st);
+
+struct Fp8Operand { const uint8_t* codes; long rows, stride; int block_rows; const float* scale; long srs, scs; };
+struct Fp8MatmulArgs {
+  Fp8Operand a, w; long K;
+  const float* bias; void* y; int y_dtype; long y_stride;
+  int* status;
+};
+bool launch_fp8_matmul(const Fp8MatmulArgs& g, cudaStream_t st);        // false: set-up failed
+
 // ---- preparation -----------------------------------------------------------------------------------
 void launch_prepare_linear(const int8_t* w, const float* sw, int N, int K, float sa, int za, int bits, float* mult,
                            int32_t* pre, float* bound, cudaStream_t st);
