@@ -264,8 +264,8 @@ mixaq_status mixaq_fp8_matmul(mixaq_ctx* ctx, const mixaq_fp8_matrix* a, const m
  * gamma and beta are binary32 [dim]; NULL stands for ones and zeros.  eps > 0.
  * The gate of row r is row r / rows_per_gate of `gate`: rows_per_gate >= rows is a gate per channel, the length of a sequence a gate
  * per sequence, 1 a gate per token; gate == NULL: ones.
- * y == NULL: x_out = x, only h is computed (gate and post do not count).  h_fp8 != NULL: h is quantized as by mixaq_fp8_quantize
- * into this matrix (block_rows 1) and `h` is not used.  pre.kind NONE: no h (h and h_fp8 NULL).
+ * y == NULL: x_out = x, only h is computed; gate, post and x_out are NULL, NONE and NULL then.  h_fp8 != NULL: h is quantized as by
+ * mixaq_fp8_quantize into this matrix (block_rows 1) in place of p->h, which is NULL then.  pre.kind NONE: no h (both NULL).
  * x_out may be x, and h may be y (same address and stride); no other outputs may overlap.  1 <= dim <= MIXAQ_NORM_MAX_DIM.
  * Pointers need the alignment of their elements; 16-byte aligned rows and a dim that is a multiple of 8 run fastest.
  * Type pairs (x, y): (F32, any), (BF16, BF16), (F16, F16).  gate_dtype: y_dtype or MIXAQ_F32. */
@@ -282,20 +282,21 @@ typedef struct {
   mixaq_norm post, pre;
   void* x_out; int64_t x_out_stride;                 /* with y only */
   void* h; int64_t h_stride;
-  const mixaq_fp8_matrix* h_fp8; int pow2;
+  int pow2;                                          /* scales of h_fp8 that are powers of two */
 } mixaq_residual_norm_params;
-mixaq_status mixaq_residual_norm_forward(mixaq_ctx* ctx, const mixaq_residual_norm_params* p, void* cuda_stream);
+mixaq_status mixaq_residual_norm_forward(mixaq_ctx* ctx, const mixaq_residual_norm_params* p, const mixaq_fp8_matrix* h_fp8 /* nullable */,
+                                         void* cuda_stream);
 
 /* Its gradients.  Of `p` are read: rows, dim, the types, x and x_stride, which are here the x_out that the forward call WROTE (its
- * x without y), y, gate, scale, post and pre.  dx_out and dh: gradients of x_out (x_dtype) and of h (y_dtype); one of the two may be
- * NULL (dx_out: nothing but h was used; dh: there is no pre norm).  Quantizing h counts as the identity.
+ * x without y; not read and may be NULL without dh), y, gate, scale, post and pre.  dx_out and dh: gradients of x_out (x_dtype) and of h
+ * (y_dtype); one of the two may be NULL (it counts as zeros).  Quantizing h counts as the identity.
  *   dx     = dx_out + J_pre^T dh                    rounded to x_dtype; the rest is computed from the unrounded sum
  *   dgate  = sum over the gate's rows of scale * dx o norm_post(y)              binary32 [gates][dim]
  *   dy     = J_post^T (scale * gate o dx)           y_dtype
  *   d*_gamma, d*_beta                               binary32 [dim], sums over the rows
- * Every output may be NULL.  dx may be dx_out, dy may be dh or y (same address and stride).  Sums over rows are added in an order that
- * depends on the sizes and the device only.  workspace: 256-byte aligned; not shared by calls that can overlap.
- * rows == 0 writes zeros to dgate's rows (none) and to the parameter gradients. */
+ * Every output may be NULL, and is where what it belongs to is missing.  dx may be dx_out, dy may be dh or y (same address and stride).
+ * Sums over rows are added in an order that depends on the sizes and the device only.  workspace: 256-byte aligned; calls that can
+ * overlap, recorded ones among them, need one each.  rows == 0 writes zeros to the parameter gradients. */
 typedef struct {
   const void* dx_out; int64_t dx_out_stride;
   const void* dh; int64_t dh_stride;

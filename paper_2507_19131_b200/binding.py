@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from types import SimpleNamespace
 from typing import Iterable, List, Optional
 
@@ -26,6 +27,7 @@ EXPORTS = [
     "mixaq_norm_forward", "mixaq_profile_end_records", "mixaq_calibrate_block_workspace_bytes", "mixaq_calibrate_block",
     "mixaq_calibrate_merge_workspace_bytes", "mixaq_calibrate_merge", "mixaq_aq_from_range", "mixaq_clear_device_status", "mixaq_selftest_wait_timeout", "mixaq_measure_mma_peak", "mixaq_set_window_elevation", "mixaq_set_reverse_selection", "mixaq_set_nvtx", "mixaq_set_workspace_guards", "mixaq_selftest_workspace_guards",
     "mixaq_fp8_quantize", "mixaq_fp8_matmul",
+    "mixaq_residual_norm_forward", "mixaq_residual_norm_backward_workspace_bytes", "mixaq_residual_norm_backward",
 ]
 
 STATUS = {0: "OK", -1: "INVALID_ARG", -2: "UNSUPPORTED_SHAPE", -3: "WORKSPACE_TOO_SMALL", -4: "CUDA_ERROR",
@@ -116,9 +118,16 @@ def lib():
         for n in ("mixaq_embed_prepared_bytes", "mixaq_embed_workspace_bytes",
                   "mixaq_block_prepared_bytes", "mixaq_merge_prepared_bytes", "mixaq_block_workspace_bytes",
                   "mixaq_merge_workspace_bytes", "mixaq_backbone_workspace_bytes",
-                  "mixaq_calibrate_block_workspace_bytes", "mixaq_calibrate_merge_workspace_bytes"):
+                  "mixaq_calibrate_block_workspace_bytes", "mixaq_calibrate_merge_workspace_bytes",
+                  "mixaq_residual_norm_backward_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
         L.mixaq_low_count.argtypes = [C.c_float, C.c_int]
+        ptr, i64 = C.c_void_p, C.c_int64
+        L.mixaq_fp8_quantize.argtypes = [ptr, ptr, C.c_int, i64, i64, i64, C.c_int, C.c_int, ptr, ptr]
+        L.mixaq_fp8_matmul.argtypes = [ptr, ptr, ptr, ptr, ptr, C.c_int, i64, ptr]
+        L.mixaq_residual_norm_forward.argtypes = [ptr, ptr, ptr, ptr]
+        L.mixaq_residual_norm_backward_workspace_bytes.argtypes = [ptr]
+        L.mixaq_residual_norm_backward.argtypes = [ptr, ptr, ptr, ptr, C.c_size_t, ptr]
         _lib = L
     return _lib
 
@@ -553,15 +562,15 @@ def backbone_forward(ctx: Context, dbb: DeviceBackbone, x0: torch.Tensor, low_ra
 
 
 # ---- row operators: e4m3 codes with block scales, their product, the norms at a sublayer's border ---------------------------------
+# Structs are packed, not built field by field: these calls are short (a matmul's host work is 12 us, 4 of them the launch).
 FP8_BLOCK = 128
 NORM_MAX_DIM = 16384
+_E4M3, _F32 = torch.float8_e4m3fn, torch.float32
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _NORM_KINDS = {"layer": 1, "rms": 2}
-
-
-class Fp8MatrixS(C.Structure):
-    _fields_ = [("codes", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("row_stride", C.c_int64), ("block_rows", C.c_int),
-                ("scale", C.c_void_p), ("scale_row_stride", C.c_int64), ("scale_col_stride", C.c_int64)]
+_FP8_MATRIX = struct.Struct("=QqqqixxxxQqq")                                       # mixaq_fp8_matrix
+_NORM_PARAMS = struct.Struct("=qiiiiQqQqQqqfxxxxixxxxQQfxxxxixxxxQQfxxxxQqQqixxxx")  # mixaq_residual_norm_params
+_NORM_GRADS = struct.Struct("=QqQqQqQqQqQQQQ")                                     # mixaq_residual_norm_grads
 
 
 def _need(ok, what: str):
@@ -569,28 +578,46 @@ def _need(ok, what: str):
         raise MixaqError(-1, what)
 
 
-def _matrix(ctx: Context, t: torch.Tensor, name: str, dtypes=_DTYPES):
-    """Checks a 2-D tensor whose rows are contiguous; returns its row stride (that of a single row counts as its length)."""
-    _need(isinstance(t, torch.Tensor) and t.dim() == 2, f"{name}: a 2-D tensor is needed")
-    _need(t.device == ctx.device, f"{name}: on {t.device}, the context's device is {ctx.device}")
-    _need(t.dtype in dtypes, f"{name}: unsupported dtype {t.dtype}")
-    rows, cols = t.shape
-    _need(cols <= 1 or t.stride(1) == 1, f"{name}: the elements of a row must be neighbours")
-    return t.stride(0) if rows > 1 else max(t.stride(0), cols)
+def _ld(ctx: Context, t: torch.Tensor, rows: int, cols: int, name: str) -> int:
+    """Row stride of a [rows, cols] tensor on the context's device whose rows are contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.device == ctx.device and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols):
+        got = f"{tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise MixaqError(-1, f"{name}: a tensor of {(rows, cols)} on {ctx.device} is needed, got {got}")
+    ld, unit = t.stride()
+    if unit != 1 and cols > 1:
+        raise MixaqError(-1, f"{name}: the elements of a row must be neighbours")
+    if rows <= 1:
+        return max(ld, cols)                  # (a single row has no stride)
+    if ld < cols:
+        raise MixaqError(-1, f"{name}: rows overlap")
+    return ld
 
 
-def _vector(ctx: Context, t: Optional[torch.Tensor], n: int, name: str):
+def _typed_ld(ctx, t, rows, cols, dtype, name) -> int:
+    ld = _ld(ctx, t, rows, cols, name)
+    if t.dtype is not dtype:
+        raise MixaqError(-1, f"{name}: {dtype} is needed, got {t.dtype}")
+    return ld
+
+
+def _vector(ctx: Context, t: Optional[torch.Tensor], n: int, name: str) -> int:
+    """Address of a contiguous float32 vector, 0 for None."""
     if t is None:
-        return None
-    _need(t.device == ctx.device and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == (n,),
-          f"{name}: a contiguous float32 vector of {n} on {ctx.device} is needed")
-    return _ptr(t)
+        return 0
+    if not (isinstance(t, torch.Tensor) and t.dtype is _F32 and t.device == ctx.device and t.dim() == 1 and t.shape[0] == n and (n <= 1 or t.stride(0) == 1)):
+        raise MixaqError(-1, f"{name}: a contiguous float32 vector of {n} on {ctx.device} is needed")
+    return t.data_ptr()
+
+
+def _stream() -> int:
+    return _raw_stream(torch.cuda.current_device()) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 class Fp8Matrix:
     """A matrix of e4m3 codes with a scale per block of block_rows x 128 (mixaq_fp8_matrix).
     codes: [rows, cols] float8_e4m3fn, 16-byte aligned, row stride a multiple of 16; scale: [ceil(rows/block_rows), ceil(cols/128)]
-    float32 in any order."""
+    float32 in any order; block_rows: 1 or 128."""
+    __slots__ = ("codes", "scale", "block_rows")
 
     def __init__(self, codes: torch.Tensor, scale: torch.Tensor, block_rows: int = 1):
         self.codes, self.scale, self.block_rows = codes, scale, block_rows
@@ -599,27 +626,34 @@ class Fp8Matrix:
     def empty(cls, rows: int, cols: int, block_rows: int, device) -> "Fp8Matrix":
         """Room for a matrix: rows padded to a multiple of 16 bytes; scales of single rows with the rows as neighbours."""
         ld = -(-cols // 16) * 16
-        codes = torch.empty((rows, ld), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+        codes = torch.empty((rows, ld), dtype=_E4M3, device=device)
+        if ld != cols:
+            codes = codes[:, :cols]
         rb, cb = -(-rows // block_rows), -(-cols // FP8_BLOCK)
-        scale = torch.empty((cb, rb), dtype=torch.float32, device=device).t() if block_rows == 1 else \
-            torch.empty((rb, cb), dtype=torch.float32, device=device)
+        scale = torch.empty_strided((rb, cb), (1, rb) if block_rows == 1 else (cb, 1), dtype=_F32, device=device)
         return cls(codes, scale, block_rows)
 
     @property
     def shape(self):
         return self.codes.shape
 
-    def struct(self, ctx: Context, name: str) -> Fp8MatrixS:
-        rows, cols = self.codes.shape if self.codes.dim() == 2 else (0, 0)
-        ld = _matrix(ctx, self.codes, name + ".codes", (torch.float8_e4m3fn,))
+    def pack(self, ctx: Context, name: str = "matrix") -> bytes:
+        """The mixaq_fp8_matrix of these tensors."""
+        codes, scale, br = self.codes, self.scale, self.block_rows
+        if br != 1 and br != FP8_BLOCK:
+            raise MixaqError(-1, f"{name}: block_rows must be 1 or {FP8_BLOCK}")
+        if not (codes.dtype is _E4M3 and scale.dtype is _F32 and codes.device == ctx.device and scale.device == ctx.device and codes.dim() == 2):
+            raise MixaqError(-1, f"{name}: 2-D float8_e4m3fn codes and float32 scales on {ctx.device} are needed")
+        rows, cols = codes.shape
+        if scale.shape != (-(-rows // br), -(-cols // FP8_BLOCK)):
+            raise MixaqError(-1, f"{name}: scales of {(-(-rows // br), -(-cols // FP8_BLOCK))} are needed, got {tuple(scale.shape)}")
+        ld, unit = codes.stride()
+        if unit != 1 and cols > 1:
+            raise MixaqError(-1, f"{name}: the codes of a row must be neighbours")
         if rows <= 1:
-            ld = -(-ld // 16) * 16            # (a single row has no stride)
-        _need(self.block_rows in (1, FP8_BLOCK), f"{name}: block_rows must be 1 or {FP8_BLOCK}")
-        want = (-(-rows // self.block_rows), -(-cols // FP8_BLOCK))
-        s = self.scale
-        _need(isinstance(s, torch.Tensor) and s.device == ctx.device and s.dtype == torch.float32 and tuple(s.shape) == want,
-              f"{name}.scale: a float32 tensor {want} on {ctx.device} is needed")
-        return Fp8MatrixS(self.codes.data_ptr(), rows, cols, ld, self.block_rows, s.data_ptr(), s.stride(0), s.stride(1))
+            ld = -(-cols // 16) * 16              # (a single row has no stride)
+        s0, s1 = scale.stride()
+        return _FP8_MATRIX.pack(codes.data_ptr(), rows, cols, ld, br, scale.data_ptr(), s0, s1)
 
     def values(self) -> torch.Tensor:
         """The float32 values that the codes stand for (a plain torch expression, for inspection)."""
@@ -632,29 +666,158 @@ def fp8_quantize(ctx: Context, x: torch.Tensor, block_rows: int = 1, transpose: 
                  out: Optional[Fp8Matrix] = None) -> Fp8Matrix:
     """mixaq_fp8_quantize: x [rows, cols] (float32, bfloat16, float16) to e4m3 codes with a scale per block of block_rows (1 or 128)
     by 128 columns; transpose: of the transposed matrix; pow2: scales that are powers of two."""
-    ld = _matrix(ctx, x, "x")
+    _need(isinstance(x, torch.Tensor) and x.dim() == 2 and x.dtype in _DTYPES, "x: a 2-D float32, bfloat16 or float16 tensor is needed")
     rows, cols = x.shape
-    _need(block_rows in (1, FP8_BLOCK), f"block_rows must be 1 or {FP8_BLOCK}")
+    ld = _ld(ctx, x, rows, cols, "x")
     r, c = (cols, rows) if transpose else (rows, cols)
     if out is None:
+        if block_rows != 1 and block_rows != FP8_BLOCK:
+            raise MixaqError(-1, f"block_rows must be 1 or {FP8_BLOCK}")
         out = Fp8Matrix.empty(r, c, block_rows, x.device)
-    _need(out.block_rows == block_rows, "out has other blocks")
-    s = out.struct(ctx, "out")
-    ctx.check(lib().mixaq_fp8_quantize(ctx.h, _ptr(x), _DTYPES[x.dtype], C.c_int64(rows), C.c_int64(cols), C.c_int64(ld),
-                                       1 if transpose else 0, 1 if pow2 else 0, C.byref(s), _stream_ptr()), "fp8_quantize")
+    elif out.block_rows != block_rows:
+        raise MixaqError(-1, "out has other blocks")
+    st = _lib.mixaq_fp8_quantize(ctx.h, x.data_ptr(), _DTYPES[x.dtype], rows, cols, ld, transpose, pow2, out.pack(ctx, "out"), _stream())
+    if st:
+        ctx.check(st, "fp8_quantize")
     return out
 
 
 def fp8_matmul(ctx: Context, a: Fp8Matrix, w: Fp8Matrix, bias: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
                y: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """mixaq_fp8_matmul: y [a.rows, w.rows] = a w^T + bias in out_dtype (float32, bfloat16, float16)."""
-    sa, sw = a.struct(ctx, "a"), w.struct(ctx, "w")
-    m, n = sa.rows, sw.rows
+    """mixaq_fp8_matmul: y [a rows, w rows] = a w^T + bias in out_dtype (float32, bfloat16, float16), or in y's type."""
+    m, n = a.codes.shape[0], w.codes.shape[0]
+    pa, pw = a.pack(ctx, "a"), w.pack(ctx, "w")
     if y is None:
-        _need(out_dtype in _DTYPES, f"unsupported out_dtype {out_dtype}")
+        if out_dtype not in _DTYPES:
+            raise MixaqError(-1, f"out_dtype: float32, bfloat16 or float16 is needed, got {out_dtype}")
         y = torch.empty((m, n), dtype=out_dtype, device=a.codes.device)
-    ld = _matrix(ctx, y, "y")
-    _need(tuple(y.shape) == (m, n), f"y: {(m, n)} is needed")
-    ctx.check(lib().mixaq_fp8_matmul(ctx.h, C.byref(sa), C.byref(sw), _vector(ctx, bias, n, "bias"), _ptr(y), _DTYPES[y.dtype],
-                                     C.c_int64(ld), _stream_ptr()), "fp8_matmul")
+        ld = n
+    else:
+        ld = _ld(ctx, y, m, n, "y")
+        _need(y.dtype in _DTYPES, f"y: float32, bfloat16 or float16 is needed, got {y.dtype}")
+    st = _lib.mixaq_fp8_matmul(ctx.h, pa, pw, _vector(ctx, bias, n, "bias"), y.data_ptr(), _DTYPES[y.dtype], ld, _stream())
+    if st:
+        ctx.check(st, "fp8_matmul")
     return y
+
+
+class Norm:
+    """A normalisation over the last axis (mixaq_norm): kind "layer" or "rms", gamma and beta float32 vectors or None, eps > 0."""
+    __slots__ = ("kind", "gamma", "beta", "eps")
+
+    def __init__(self, kind: str, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: float = 1e-5):
+        if kind not in _NORM_KINDS:
+            raise MixaqError(-1, f"norm kind {kind!r}: 'layer' or 'rms' is needed")
+        self.kind, self.gamma, self.beta, self.eps = kind, gamma, beta, eps
+
+
+def _norm_fields(ctx: Context, norm: Optional[Norm], dim: int, name: str):
+    if norm is None:
+        return 0, 0, 0, 0.0
+    return _NORM_KINDS[norm.kind], _vector(ctx, norm.gamma, dim, name + ".gamma"), _vector(ctx, norm.beta, dim, name + ".beta"), norm.eps
+
+
+def _gate_fields(ctx: Context, gate: Optional[torch.Tensor], rows_per_gate: Optional[int], rows: int, dim: int, y_dtype):
+    """(address, dtype, stride, rows_per_gate, gates) of a gate [dim] or [gates, dim]."""
+    if gate is None:
+        return 0, 0, 0, 0, 0
+    if gate.dim() == 1:
+        gate = gate.unsqueeze(0)
+    gates = gate.shape[0]
+    if rows_per_gate is None:
+        _need(gates > 0 and rows % gates == 0, f"gate: {gates} gates for {rows} rows need rows_per_gate")
+        rows_per_gate = max(rows // gates, 1)
+    _need(rows_per_gate >= 1 and gates == max(-(-rows // rows_per_gate), min(gates, 1)), f"gate: {gates} gates of {rows_per_gate} rows each are not {rows} rows")
+    ld = _ld(ctx, gate, gates, dim, "gate")
+    _need(gate.dtype is y_dtype or gate.dtype is _F32, f"gate: {y_dtype} or float32 is needed, got {gate.dtype}")
+    return gate.data_ptr(), _DTYPES[gate.dtype], ld, rows_per_gate, gates
+
+
+def residual_norm_forward(ctx: Context, x: torch.Tensor, y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                          rows_per_gate: Optional[int] = None, scale: float = 1.0, post: Optional[Norm] = None, pre: Optional[Norm] = None,
+                          h_dtype=None, fp8: bool = False, pow2: bool = False, x_out: Optional[torch.Tensor] = None, h=None):
+    """mixaq_residual_norm_forward on [rows, dim] matrices: x' = x + scale * gate * post(y), h = pre(x').  Returns a namespace with x (x'
+    rounded to x's type; x itself without y) and h (None without pre; an Fp8Matrix with fp8).
+    gate: [dim], or [gates, dim] for rows_per_gate consecutive rows each (by default the rows are dealt evenly).  h_dtype: type of h where
+    y does not give it (default: x's).  x_out, h: tensors (for fp8 an Fp8Matrix) to write to; x_out may be x, h may be y."""
+    _need(isinstance(x, torch.Tensor) and x.dim() == 2 and x.dtype in _DTYPES, "x: a 2-D float32, bfloat16 or float16 tensor is needed")
+    rows, dim = x.shape
+    x_ld = _ld(ctx, x, rows, dim, "x")
+    y_dtype = y.dtype if y is not None else x.dtype if h_dtype is None else h_dtype
+    _need(y_dtype in _DTYPES and (h_dtype is None or h_dtype is y_dtype), "y and h: float32, bfloat16 or float16, both the same, are needed")
+    _need(pre is not None or (h is None and not fp8), "h without a pre norm")
+    y_at = y_ld = out_at = out_ld = h_at = h_ld = 0
+    new_x = x
+    if y is not None:
+        y_at, y_ld = y.data_ptr(), _ld(ctx, y, rows, dim, "y")
+        if x_out is None:
+            x_out = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
+        new_x, out_at, out_ld = x_out, x_out.data_ptr(), _typed_ld(ctx, x_out, rows, dim, x.dtype, "x_out")
+    else:
+        _need(x_out is None, "x_out without y")
+    packed = None
+    if pre is not None:
+        if fp8:
+            if h is None:
+                h = Fp8Matrix.empty(rows, dim, 1, x.device)
+            packed = h.pack(ctx, "h")
+        else:
+            if h is None:
+                h = torch.empty((rows, dim), dtype=y_dtype, device=x.device)
+            h_at, h_ld = h.data_ptr(), _typed_ld(ctx, h, rows, dim, y_dtype, "h")
+    g_at, g_dtype, g_ld, per, _ = _gate_fields(ctx, gate, rows_per_gate, rows, dim, y_dtype)
+    p = _NORM_PARAMS.pack(rows, dim, _DTYPES[x.dtype], _DTYPES[y_dtype], g_dtype, x.data_ptr(), x_ld, y_at, y_ld, g_at, g_ld, per, scale,
+                          *_norm_fields(ctx, post, dim, "post"), *_norm_fields(ctx, pre, dim, "pre"), out_at, out_ld, h_at, h_ld, pow2)
+    st = _lib.mixaq_residual_norm_forward(ctx.h, p, packed, _stream())
+    if st:
+        ctx.check(st, "residual_norm_forward")
+    return SimpleNamespace(x=new_x, h=h)
+
+
+def residual_norm_backward(ctx: Context, x: Optional[torch.Tensor], y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                           rows_per_gate: Optional[int] = None, scale: float = 1.0, post: Optional[Norm] = None, pre: Optional[Norm] = None,
+                           dx_out: Optional[torch.Tensor] = None, dh: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """mixaq_residual_norm_backward: the gradients of residual_norm_forward.  x: the x that the forward call returned (None without dh);
+    the other arguments as there; dx_out, dh: gradients of the returned x and h.  Returns a namespace with dx, dy, dgate ([gates, dim]
+    float32) and dpost_gamma, dpost_beta, dpre_gamma, dpre_beta (float32), None where the forward call had no such argument.
+    workspace: a uint8 tensor that the caller keeps (by default one is allocated)."""
+    like = dx_out if dx_out is not None else x
+    _need(isinstance(like, torch.Tensor) and like.dim() == 2 and like.dtype in _DTYPES, "dx_out or x: a 2-D float32, bfloat16 or float16 tensor is needed")
+    _need(dh is None or pre is not None, "dh without a pre norm")
+    _need(dh is None or x is not None, "dh needs x")
+    rows, dim = like.shape
+    x_dtype = like.dtype
+    y_dtype = y.dtype if y is not None else dh.dtype if dh is not None else x_dtype
+    _need(y_dtype in _DTYPES, f"y: float32, bfloat16 or float16 is needed, got {y_dtype}")
+    dev = like.device
+
+    def place(t, dtype, name):
+        return (0, 0) if t is None else (t.data_ptr(), _typed_ld(ctx, t, rows, dim, dtype, name))
+
+    g_at, g_dtype, g_ld, per, gates = _gate_fields(ctx, gate, rows_per_gate, rows, dim, y_dtype)
+    out = SimpleNamespace(dx=torch.empty((rows, dim), dtype=x_dtype, device=dev), dy=None, dgate=None,
+                          dpost_gamma=None, dpost_beta=None, dpre_gamma=None, dpre_beta=None)
+    if y is not None:
+        out.dy = torch.empty((rows, dim), dtype=y_dtype, device=dev)
+    if gate is not None:
+        out.dgate = torch.empty((gates, dim), dtype=_F32, device=dev)
+        if rows == 0:
+            out.dgate.zero_()
+    wanted = [name for norm, at in ((post, "dpost_"), (pre, "dpre_")) if norm is not None
+              for part, name in ((norm.gamma, at + "gamma"), (norm.beta, at + "beta")) if part is not None]
+    vectors = torch.empty((max(len(wanted), 1), dim), dtype=_F32, device=dev)
+    for i, name in enumerate(wanted):
+        setattr(out, name, vectors[i])
+    p = _NORM_PARAMS.pack(rows, dim, _DTYPES[x_dtype], _DTYPES[y_dtype], g_dtype, *place(x, x_dtype, "x"), *place(y, y_dtype, "y"), g_at, g_ld, per,
+                          scale, *_norm_fields(ctx, post, dim, "post"), *_norm_fields(ctx, pre, dim, "pre"), 0, 0, 0, 0, 0)
+    at = [getattr(out, name).data_ptr() if getattr(out, name) is not None else 0 for name in ("dpost_gamma", "dpost_beta", "dpre_gamma", "dpre_beta")]
+    g = _NORM_GRADS.pack(*place(dx_out, x_dtype, "dx_out"), *place(dh, y_dtype, "dh"), out.dx.data_ptr(), dim,
+                         out.dy.data_ptr() if y is not None else 0, dim, out.dgate.data_ptr() if gate is not None else 0, dim, *at)
+    need = _lib.mixaq_residual_norm_backward_workspace_bytes(p)
+    if workspace is None:
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    _need(workspace.device == ctx.device and workspace.is_contiguous(), f"workspace: a contiguous tensor on {ctx.device} is needed")
+    st = _lib.mixaq_residual_norm_backward(ctx.h, p, g, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream())
+    if st:
+        ctx.check(st, "residual_norm_backward")
+    return out

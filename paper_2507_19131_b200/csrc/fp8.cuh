@@ -30,6 +30,17 @@ template <class T> __device__ __forceinline__ void load_some8(const T* p, int n,
 #pragma unroll
   for (int i = 0; i < 8; ++i) r.v[i] = i < n ? __ldg(p + i) : from_f32<T>(0.0f);
 }
+// loads of memory that the kernel itself may write later (rows updated in place)
+template <class T> __device__ __forceinline__ void load_row8(const T* p, bool vec, int n, Vec8<T>& r) {
+  if (vec && n >= 8) {
+    uint4* d = reinterpret_cast<uint4*>(&r);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(Vec8<T>) / 16; ++i) d[i] = reinterpret_cast<const uint4*>(p)[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.v[i] = i < n ? p[i] : from_f32<T>(0.0f);
+  }
+}
 template <class T> __device__ __forceinline__ void unpack8(const Vec8<T>& r, float (&f)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = to_f32(r.v[i]);

@@ -174,6 +174,28 @@ struct Fp8MatmulArgs {
 };
 bool launch_fp8_matmul(const Fp8MatmulArgs& g, cudaStream_t st);        // false: set-up failed
 
+struct NormSpec { int kind; const float *gamma, *beta; float eps; };          // kind: values of mixaq_norm_kind
+struct ResNormArgs {
+  long rows; int dim, x_dtype, y_dtype;
+  const void* x; long x_stride; const void* y; long y_stride;                 // y nullable
+  const void* gate; long gate_stride, rows_per_gate; bool gate_f32;           // nullable
+  float scale;
+  NormSpec post, pre;
+  void* x_out; long x_out_stride; void* h; long h_stride;                     // h: of the sublayers' type, or
+  uint8_t* codes; long code_stride; float* h_scale; long srs, scs; bool pow2;  // codes (h is null then)
+};
+struct ResNormGradArgs {
+  const void* dx_out; long dx_out_stride; const void* dh; long dh_stride;     // nullable
+  void* dx; long dx_stride; void* dy; long dy_stride;                         // nullable, as all that follows
+  float* dgate; long dgate_stride;
+  float* vec[4];                                                              // dpost_gamma, dpost_beta, dpre_gamma, dpre_beta
+  float* workspace;
+};
+constexpr int NORM_MAX_DIM = 16384;
+void launch_residual_norm(const ResNormArgs& a, cudaStream_t st);
+size_t residual_norm_backward_floats(long rows, int dim, bool gate_per_sequence);   // of the workspace
+void launch_residual_norm_backward(const ResNormArgs& a, const ResNormGradArgs& g, cudaStream_t st);
+
 // ---- preparation -----------------------------------------------------------------------------------
 void launch_prepare_linear(const int8_t* w, const float* sw, int N, int K, float sa, int za, int bits, float* mult,
                            int32_t* pre, float* bound, cudaStream_t st);

@@ -46,6 +46,45 @@ Fp8Operand operand(const mixaq_fp8_matrix& m) {
   return {m.codes, (long)m.rows, (long)m.row_stride, m.block_rows, m.scale, (long)m.scale_row_stride, (long)m.scale_col_stride};
 }
 
+// ---- norms ----
+bool norm_ok(const mixaq_norm& n) {
+  if (n.kind == MIXAQ_NORM_NONE) return true;
+  return (n.kind == MIXAQ_NORM_LAYER || n.kind == MIXAQ_NORM_RMS) && n.eps > 0.f && n.eps <= 3.402823466e38f && aligned_to(n.gamma, 4) && aligned_to(n.beta, 4);
+}
+NormSpec norm_spec(const mixaq_norm& n) { return {(int)n.kind, n.gamma, n.beta, n.eps}; }
+
+// a matrix of `size`-byte elements that has to be there: aligned, rows that do not overlap
+bool rows_ok(const void* p, int64_t stride, int64_t dim, size_t size) { return p && aligned_to(p, size) && stride >= dim && stride < MAX_STRIDE; }
+
+// what the forward and the backward call have in common
+mixaq_status check_residual_norm(mixaq_ctx* ctx, const mixaq_residual_norm_params* p) {
+  if (!p) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: params are NULL");
+  if (p->rows < 0 || p->dim < 1) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: rows must not be negative, dim at least 1");
+  if (p->rows > MAX_EXTENT || p->dim > MIXAQ_NORM_MAX_DIM) return fail(ctx, MIXAQ_UNSUPPORTED_SHAPE, "residual_norm: too many rows, or dim beyond MIXAQ_NORM_MAX_DIM");
+  if (!dtype_ok(p->x_dtype) || !dtype_ok(p->y_dtype)) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: unknown dtype");
+  if (p->x_dtype != MIXAQ_F32 && p->x_dtype != p->y_dtype) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: a 16-bit x needs y of its own type");
+  if (!norm_ok(p->post) || !norm_ok(p->pre)) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: norm kind unknown, eps not positive, or gamma or beta not 4-byte aligned");
+  if (!p->y && (p->gate || p->post.kind != MIXAQ_NORM_NONE)) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: gate or post norm without y");
+  if (p->gate) {
+    if (p->gate_dtype != p->y_dtype && p->gate_dtype != MIXAQ_F32) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: gate_dtype must be y_dtype or MIXAQ_F32");
+    if (p->rows_per_gate < 1) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: rows_per_gate must be at least 1");
+    if (p->gate_stride < 0 || p->gate_stride >= MAX_STRIDE || !aligned_to(p->gate, dtype_size(p->gate_dtype)))
+      return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: gate stride out of range, or gate not aligned to its elements");
+  }
+  return MIXAQ_OK;
+}
+
+ResNormArgs norm_args(const mixaq_residual_norm_params& p) {
+  ResNormArgs a = {};
+  a.rows = p.rows; a.dim = p.dim; a.x_dtype = p.x_dtype; a.y_dtype = p.y_dtype;
+  a.x = p.x; a.x_stride = p.x_stride; a.y = p.y; a.y_stride = p.y_stride;
+  a.gate = p.gate; a.gate_stride = p.gate_stride; a.gate_f32 = p.gate_dtype == MIXAQ_F32;
+  a.rows_per_gate = !p.gate || p.rows_per_gate > p.rows ? p.rows : p.rows_per_gate;       // (rows > 0 here)
+  a.scale = p.scale; a.post = norm_spec(p.post); a.pre = norm_spec(p.pre);
+  return a;
+}
+bool gate_per_sequence(const mixaq_residual_norm_params& p) { return p.gate && p.rows_per_gate > 1 && p.rows_per_gate < p.rows; }
+
 }  // namespace
 
 extern "C" {
@@ -107,6 +146,97 @@ mixaq_status mixaq_fp8_matmul(mixaq_ctx* ctx, const mixaq_fp8_matrix* a, const m
   ctx->launches = g_launches;
   if (!ok) { cudaGetLastError(); return fail(ctx, MIXAQ_INTERNAL, "fp8_matmul: launch set-up failed (tensor map, shared memory or registers)"); }
   return check_cuda(ctx, "fp8_matmul");
+}
+
+mixaq_status mixaq_residual_norm_forward(mixaq_ctx* ctx, const mixaq_residual_norm_params* p, const mixaq_fp8_matrix* h_fp8, void* cuda_stream) {
+  if (!ctx) return MIXAQ_INVALID_ARG;
+  ctx->launches = 0;
+  if (mixaq_status s = check_residual_norm(ctx, p)) return s;
+  const bool pre = p->pre.kind != MIXAQ_NORM_NONE;
+  if (pre ? !p->h == !h_fp8 : p->h || h_fp8) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: a pre norm needs h or h_fp8, one of them; none takes neither");
+  if (!pre && !p->y) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: neither y nor a pre norm");
+  if (!p->y && p->x_out) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: x_out without y");
+  if (h_fp8) {
+    if (h_fp8->rows != p->rows || h_fp8->cols != p->dim || h_fp8->block_rows != 1) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: h_fp8 has another shape than x, or block_rows other than 1");
+    if (mixaq_status s = check_matrix(ctx, h_fp8, true)) return s;
+  }
+  if (p->rows == 0) return MIXAQ_OK;
+  const size_t xs = dtype_size(p->x_dtype), ys = dtype_size(p->y_dtype);
+  if (!rows_ok(p->x, p->x_stride, p->dim, xs) || (p->y && (!rows_ok(p->y, p->y_stride, p->dim, ys) || !rows_ok(p->x_out, p->x_out_stride, p->dim, xs))) ||
+      (p->h && !rows_ok(p->h, p->h_stride, p->dim, ys)))
+    return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: x, y, x_out or h missing, not aligned to its elements, or with a stride below dim");
+  if ((p->x_out == p->x && p->x_out_stride != p->x_stride) || (p->h && p->h == p->y && p->h_stride != p->y_stride) ||
+      (p->h && (p->h == p->x || p->h == p->x_out)) || (p->y && p->x_out == p->y))
+    return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: outputs overlap");
+  if (mixaq_status s = check_device(ctx)) return s;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  ResNormArgs a = norm_args(*p);
+  a.x_out = p->x_out; a.x_out_stride = p->x_out_stride; a.h = p->h; a.h_stride = p->h_stride;
+  if (h_fp8) {
+    a.codes = h_fp8->codes; a.code_stride = h_fp8->row_stride; a.h_scale = h_fp8->scale;
+    a.srs = h_fp8->scale_row_stride; a.scs = h_fp8->scale_col_stride; a.pow2 = p->pow2 != 0;
+  }
+  g_launches = 0;
+  try {
+    ProfScope scope(ctx, PC_RES_NORM, st);
+    launch_residual_norm(a, st);
+  } catch (...) { return fail(ctx, MIXAQ_INTERNAL, "residual_norm_forward: out of host memory"); }
+  ctx->launches = g_launches;
+  return check_cuda(ctx, "residual_norm_forward");
+}
+
+size_t mixaq_residual_norm_backward_workspace_bytes(const mixaq_residual_norm_params* p) {
+  if (!p || p->rows < 0 || p->rows > MAX_EXTENT || p->dim < 1 || p->dim > MIXAQ_NORM_MAX_DIM) return 0;
+  return residual_norm_backward_floats(p->rows, p->dim, gate_per_sequence(*p)) * sizeof(float);
+}
+
+mixaq_status mixaq_residual_norm_backward(mixaq_ctx* ctx, const mixaq_residual_norm_params* p, const mixaq_residual_norm_grads* g,
+                                          void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (!ctx) return MIXAQ_INVALID_ARG;
+  ctx->launches = 0;
+  if (mixaq_status s = check_residual_norm(ctx, p)) return s;
+  if (!g) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm_backward: grads are NULL");
+  const bool pre = p->pre.kind != MIXAQ_NORM_NONE, post = p->post.kind != MIXAQ_NORM_NONE;
+  float* const vec[4] = {g->dpost_gamma, g->dpost_beta, g->dpre_gamma, g->dpre_beta};
+  if ((!pre && (g->dh || vec[2] || vec[3])) || (!post && (vec[0] || vec[1])) || (!p->y && g->dy) || (!p->gate && g->dgate))
+    return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm_backward: a gradient of something that is missing");
+  for (const float* v : vec) if (!aligned_to(v, 4)) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm_backward: parameter gradients must be 4-byte aligned");
+  if (p->rows > 0) {
+    if (!g->dx_out && !g->dh) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm_backward: neither dx_out nor dh");
+    const size_t xs = dtype_size(p->x_dtype), ys = dtype_size(p->y_dtype);
+    if ((g->dh && !rows_ok(p->x, p->x_stride, p->dim, xs)) || (p->y && !rows_ok(p->y, p->y_stride, p->dim, ys)) ||
+        (g->dx_out && !rows_ok(g->dx_out, g->dx_out_stride, p->dim, xs)) || (g->dh && !rows_ok(g->dh, g->dh_stride, p->dim, ys)) ||
+        (g->dx && !rows_ok(g->dx, g->dx_stride, p->dim, xs)) || (g->dy && !rows_ok(g->dy, g->dy_stride, p->dim, ys)) ||
+        (g->dgate && !rows_ok(g->dgate, g->dgate_stride, p->dim, 4)))
+      return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm_backward: a matrix is missing, not aligned to its elements, or has a stride below dim");
+    if ((g->dx && g->dx == g->dx_out && g->dx_stride != g->dx_out_stride) || (g->dy && g->dy == g->dh && g->dy_stride != g->dh_stride) ||
+        (g->dy && g->dy == p->y && g->dy_stride != p->y_stride) ||
+        (g->dx && (g->dx == p->x || g->dx == p->y || g->dx == g->dh || g->dx == g->dy)) || (g->dy && (g->dy == p->x || g->dy == g->dx_out)))
+      return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm_backward: outputs overlap");
+    if (gate_per_sequence(*p) && ceil_div(p->rows, p->rows_per_gate) * ceil_div(p->dim, 256) > MAX_EXTENT)
+      return fail(ctx, MIXAQ_UNSUPPORTED_SHAPE, "residual_norm_backward: too many gates");
+    if (!workspace || !aligned_to(workspace, 256)) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm_backward: workspace is NULL or not 256-byte aligned");
+    if (mixaq_residual_norm_backward_workspace_bytes(p) > workspace_bytes) return fail(ctx, MIXAQ_WORKSPACE_TOO_SMALL, "residual_norm_backward: workspace too small");
+  }
+  if (mixaq_status s = check_device(ctx)) return s;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  g_launches = 0;
+  if (p->rows == 0) {
+    for (float* v : vec) if (v) cudaMemsetAsync(v, 0, (size_t)p->dim * sizeof(float), st);
+    return check_cuda(ctx, "residual_norm_backward");
+  }
+  ResNormGradArgs a;
+  a.dx_out = g->dx_out; a.dx_out_stride = g->dx_out_stride; a.dh = g->dh; a.dh_stride = g->dh_stride;
+  a.dx = g->dx; a.dx_stride = g->dx_stride; a.dy = g->dy; a.dy_stride = g->dy_stride;
+  a.dgate = g->dgate; a.dgate_stride = g->dgate_stride;
+  for (int i = 0; i < 4; ++i) a.vec[i] = vec[i];
+  a.workspace = static_cast<float*>(workspace);
+  try {
+    ProfScope scope(ctx, PC_RES_NORM, st);
+    launch_residual_norm_backward(norm_args(*p), a, st);
+  } catch (...) { return fail(ctx, MIXAQ_INTERNAL, "residual_norm_backward: out of host memory"); }
+  ctx->launches = g_launches;
+  return check_cuda(ctx, "residual_norm_backward");
 }
 
 }  // extern "C"
