@@ -26,58 +26,119 @@ constexpr int A_BYTES = BM * BK;
 constexpr int EPI_WARPS = 8, FIRST_EPI = 4, THREADS = 32 * (FIRST_EPI + EPI_WARPS);
 constexpr int STAGING = 2048;                  // bytes of an epilogue warp's store buffer: 32 rows of 64
 constexpr int MAX_SPLIT = 8;
-constexpr int MAX_ACC = 4, MAX_RING = 8;
-__host__ __device__ constexpr int num_acc(int bn) { return bn == 256 ? 2 : MAX_ACC; }
-__host__ __device__ constexpr int ring_stages(int bn) { return bn == 256 ? 4 : bn == 128 ? 6 : MAX_RING; }
-__host__ __device__ constexpr int tmem_cols(int bn) { return num_acc(bn) * bn; }
-__host__ __device__ constexpr int stage_bytes(int bn) { return A_BYTES + bn * BK; }
-// Wide tiles keep 128 sums a thread: the side warpgroup gives up registers for them (4 x 72 + 8 x 216 of 12 x 168).
+constexpr int MAX_SLOTS = 4, MAX_RING = 8;
+// Tiles of 256 columns belong to pairs of CTAs (cta_group::2): 256 rows x 256 columns, 128 rows a CTA, each CTA loading its own rows of a
+// and half of the weights' rows.  The others are a CTA's own.
+__host__ __device__ constexpr bool paired(int bn) { return bn == 256; }
+// Accumulators ("slots") in tensor memory: a pair's tile is multiplied in two halves of 128 columns that are committed one by one, so
+// that four slots take turns and the sums of one half are read while the other one is multiplied.
+__host__ __device__ constexpr int halves(int bn) { return paired(bn) ? 2 : 1; }
+__host__ __device__ constexpr int slot_cols(int bn) { return bn / halves(bn); }
+__host__ __device__ constexpr int tmem_cols(int bn) { return MAX_SLOTS * slot_cols(bn); }
+__host__ __device__ constexpr int w_rows(int bn) { return paired(bn) ? bn / 2 : bn; }          // rows of the weights that a CTA loads
+__host__ __device__ constexpr int stage_bytes(int bn) { return A_BYTES + w_rows(bn) * BK; }
+__host__ __device__ constexpr int ring_stages(int bn) { return bn >= 128 ? 6 : MAX_RING; }
+// Pairs keep 128 sums a thread: the side warpgroup gives up registers for them (4 x 72 + 8 x 216 of 12 x 168).
 constexpr int SIDE_REGS = 72, EPI_REGS = 216;
-__host__ __device__ constexpr bool exchanges_registers(int bn) { return bn == 256; }
-constexpr int NUM_BARS = 2 * MAX_RING + 3 * MAX_ACC + 1;        // stage full, empty; accumulator full, empty, column scales; drain
+// Scales come from memory long before their k-block: a latency of 800 cycles out of the L2 and 1 500 out of memory stands against 256 to
+// 512 cycles of a k-block (read two k-blocks ahead, every tile width took 750 cycles a k-block).  AHEAD k-blocks are under way.
+constexpr int AHEAD = 8;
+// stage full, empty; slot full, empty; column scales full, empty; drain
+constexpr int NUM_BARS = 2 * MAX_RING + 2 * MAX_SLOTS + 2 * AHEAD + 1;
 
-__host__ __device__ constexpr int smem_total(int bn) {
-  return ring_stages(bn) * stage_bytes(bn) + EPI_WARPS * STAGING + num_acc(bn) * bn * 4 + NUM_BARS * 8 + 16;
+__host__ __device__ constexpr int smem_total(int bn, bool cols) {
+  return ring_stages(bn) * stage_bytes(bn) + EPI_WARPS * STAGING + (cols ? AHEAD * bn * 4 : 0) + NUM_BARS * 8 + 16;
 }
 
 struct Params {
   Fp8MatmulArgs g;
   int M, N, k_blocks;
-  int m_tiles, n_tiles, tiles, split;          // split: CTAs of a cluster that share a tile (1: no cluster)
+  int m_tiles, n_tiles, tiles;                 // (rows of a pair's tile: 256)
+  int split;                                   // CTAs of a cluster that share a tile's k-blocks (1: none)
 };
 
+template <bool PAIR>
 __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+  if constexpr (PAIR)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
-// 16 columns of the warp's 32 rows, one row per thread; valid after tmem_wait16
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
-        "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
-      : "r"(taddr) : "memory");
+// arrival, when the MMAs issued so far are done, on a barrier of this CTA (of a pair: on that of both)
+template <bool PAIR>
+__device__ __forceinline__ void commit(uint32_t bar) {
+  if constexpr (PAIR)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+  else
+    mma_commit(bar);
+}
+// the same place in the shared memory of CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  return a;
+}
+// a TMA load into this CTA's shared memory that counts on a barrier of the pair's first CTA
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// An arrival on another CTA's barrier that hands over tensor memory only (tcgen05 fences order that): a release at cluster scope would wait
+// for all memory operations of the thread, the scales in flight among them, and doubled the time of a k-block.
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void tmem_alloc(uint32_t holder, uint32_t cols) {
+  if constexpr (PAIR) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(holder), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(holder), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+}
+template <bool PAIR>
+__device__ __forceinline__ void tmem_dealloc(uint32_t base, uint32_t cols) {
+  if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols) : "memory");
+  else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols) : "memory");
+}
+// N columns (8, 16 or 32) of the warp's 32 rows, one row per thread; valid after tmem_wait
+template <int N>
+__device__ __forceinline__ void tmem_ld_rows(uint32_t taddr, float (&r)[N]) {
+  if constexpr (N == 8) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]) : "r"(taddr));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 16)
+      asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+          : "=f"(r[i]), "=f"(r[i + 1]), "=f"(r[i + 2]), "=f"(r[i + 3]), "=f"(r[i + 4]), "=f"(r[i + 5]), "=f"(r[i + 6]), "=f"(r[i + 7]),
+            "=f"(r[i + 8]), "=f"(r[i + 9]), "=f"(r[i + 10]), "=f"(r[i + 11]), "=f"(r[i + 12]), "=f"(r[i + 13]), "=f"(r[i + 14]), "=f"(r[i + 15])
+          : "r"(taddr + (uint32_t)i));
+  }
 }
 // waits for all loads; the registers pass through so that no use of them is scheduled ahead of it
-__device__ __forceinline__ void tmem_wait16(float* r) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-      : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),
-        "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]) :: "memory");
+template <int N>
+__device__ __forceinline__ void tmem_wait(float (&r)[N]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; i += 8)
+    asm volatile("" : "+f"(r[i]), "+f"(r[i + 1]), "+f"(r[i + 2]), "+f"(r[i + 3]), "+f"(r[i + 4]), "+f"(r[i + 5]), "+f"(r[i + 6]), "+f"(r[i + 7]));
 }
-__device__ __forceinline__ void pass_through16(float* r) {
-  asm volatile("" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),
-        "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]));
+
+__device__ __forceinline__ void cp_async4(uint32_t dst, const float* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 __device__ __forceinline__ float4 ld_cluster(uint32_t addr, uint32_t rank) {
-  uint32_t a;
+  const uint32_t a = cluster_addr(addr, rank);
   float4 v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
   return v;
 }
@@ -175,15 +236,18 @@ __device__ __forceinline__ void tile_at(const Params& p, int t, int& mt, int& nt
 template <int BN, bool COLSCALE>
 __global__ void __launch_bounds__(THREADS, 1)
 k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ Params p) {
-  constexpr int N_ACC = num_acc(BN), RING = ring_stages(BN), STAGE = stage_bytes(BN), COLS = BN / 2;
+  constexpr bool PAIR = paired(BN);
+  constexpr int HALVES = halves(BN), SLOT_COLS = slot_cols(BN), RING = ring_stages(BN), STAGE = stage_bytes(BN), COLS = BN / 2;
+  constexpr int SLOT_WARPS = EPI_WARPS / HALVES;              // epilogue warps that read a slot
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;     // swizzled tiles need 1024-byte alignment
   uint8_t* const smem = smem_raw + (base - raw);
   uint8_t* const staging = smem + RING * STAGE;
-  float* const col_scales = reinterpret_cast<float*>(staging + EPI_WARPS * STAGING);      // [N_ACC][BN]
-  uint64_t* const bars = reinterpret_cast<uint64_t*>(col_scales + N_ACC * BN);
+  float* const col_scales = reinterpret_cast<float*>(staging + EPI_WARPS * STAGING);      // [AHEAD][BN]
+  uint64_t* const bars = reinterpret_cast<uint64_t*>(col_scales + (COLSCALE ? AHEAD * BN : 0));
   const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8u * MAX_RING, bar_tfull = bar_empty + 8u * MAX_RING;
-  const uint32_t bar_tempty = bar_tfull + 8u * MAX_ACC, bar_cols = bar_tempty + 8u * MAX_ACC, bar_drain = bar_cols + 8u * MAX_ACC;
+  const uint32_t bar_tempty = bar_tfull + 8u * MAX_SLOTS, bar_cfull = bar_tempty + 8u * MAX_SLOTS, bar_cempty = bar_cfull + 8u * AHEAD;
+  const uint32_t bar_drain = bar_cempty + 8u * AHEAD;
   uint32_t* const tmem_holder = reinterpret_cast<uint32_t*>(bars + NUM_BARS);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -195,32 +259,33 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
   }
   if (tid == 0) {
     for (int s = 0; s < RING; ++s) { mbar_init(bar_full + 8u * s, 1u); mbar_init(bar_empty + 8u * s, 1u); }
-    for (int a = 0; a < N_ACC; ++a) {
-      mbar_init(bar_tfull + 8u * a, 1u); mbar_init(bar_tempty + 8u * a, EPI_WARPS); mbar_init(bar_cols + 8u * a, 1u);
+    for (int a = 0; a < MAX_SLOTS; ++a) {
+      mbar_init(bar_tfull + 8u * a, 1u); mbar_init(bar_tempty + 8u * a, SLOT_WARPS * (PAIR ? 2u : 1u));
     }
+    for (int a = 0; a < AHEAD; ++a) { mbar_init(bar_cfull + 8u * a, 32u); mbar_init(bar_cempty + 8u * a, EPI_WARPS); }
     mbar_init(bar_drain, 1u);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 2) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                 ::"r"(smem_u32(tmem_holder)), "r"((uint32_t)tmem_cols(BN)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
+  if (warp == 2) tmem_alloc<PAIR>(smem_u32(tmem_holder), (uint32_t)tmem_cols(BN));
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if (PAIR) cluster_sync();                    // the other CTA's barriers are ready, too
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_base = *tmem_holder;
   griddep_wait();                              // operands, scales and y may belong to earlier kernels
   griddep_launch();
-  if (exchanges_registers(BN) && warp < FIRST_EPI) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(SIDE_REGS));
+  if (PAIR && warp < FIRST_EPI) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(SIDE_REGS));
 
-  // this CTA's tiles and, in a cluster, its share of the k-blocks
-  const int rank = p.split > 1 ? (int)(blockIdx.x % (unsigned)p.split) : 0;
-  const int first = (int)(blockIdx.x / (unsigned)p.split), step = (int)(gridDim.x / (unsigned)p.split);
-  const int kb0 = (int)((long)p.k_blocks * rank / p.split), kb1 = (int)((long)p.k_blocks * (rank + 1) / p.split);
+  // this CTA's tiles and, where a cluster divides them, its share of the k-blocks
+  const int per_cluster = PAIR ? 2 : p.split, rank = (int)(blockIdx.x % (unsigned)per_cluster);
+  const int first = (int)(blockIdx.x / (unsigned)per_cluster), step = (int)(gridDim.x / (unsigned)per_cluster);
+  const int kb0 = PAIR ? 0 : (int)((long)p.k_blocks * rank / p.split), kb1 = PAIR ? p.k_blocks : (int)((long)p.k_blocks * (rank + 1) / p.split);
+  const int row_off = PAIR ? rank * BM : 0;    // of this CTA's rows in a tile
+  constexpr int TILE_M = PAIR ? 2 * BM : BM;
 
   if (warp == 0) {
+    // ---- TMA ----
     const bool leader = elect_one();
     Ring rp;
     bool ok = true;
@@ -232,108 +297,148 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         if (!mbar_wait_warp(bar_empty + o, rp.pass ^ 1u, abort_flag)) { ok = false; break; }
         ++fills;
         if (leader) {
-          mbar_arrive_expect_tx(bar_full + o, (uint32_t)STAGE);
-          tma_load_2d(sa, &tmA, kb * BK, mt * BM, bar_full + o);
-          tma_load_2d(sa + A_BYTES, &tmW, kb * BK, nt * BN, bar_full + o);
+          if constexpr (PAIR) {
+            // both CTAs' bytes count on the first one's barrier; of each half of the columns a CTA has 64 rows
+            const uint32_t full = cluster_addr(bar_full + o, 0);
+            if (rank == 0) mbar_arrive_expect_tx(bar_full + o, 2u * (uint32_t)STAGE);
+            tma_load_pair(sa, &tmA, kb * BK, mt * TILE_M + row_off, full);
+            tma_load_pair(sa + A_BYTES, &tmW, kb * BK, nt * BN + rank * 64, full);
+            tma_load_pair(sa + A_BYTES + 64 * BK, &tmW, kb * BK, nt * BN + 128 + rank * 64, full);
+          } else {
+            mbar_arrive_expect_tx(bar_full + o, (uint32_t)STAGE);
+            tma_load_2d(sa, &tmA, kb * BK, mt * BM, bar_full + o);
+            tma_load_2d(sa + A_BYTES, &tmW, kb * BK, nt * BN, bar_full + o);
+          }
         }
         __syncwarp();
       }
     }
-  } else if (warp == 1) {
+  } else if (warp == 1 && (!PAIR || rank == 0)) {
+    // ---- MMA ----
     const bool leader = elect_one();
     // D binary32 (1 at bit 4), A and B e4m3 (0 at bits 7 and 10), N / 8, M / 16
-    const uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+    const uint32_t idesc = (1u << 4) | ((uint32_t)(SLOT_COLS >> 3) << 17) | ((uint32_t)(TILE_M >> 4) << 24);
     const uint64_t adesc0 = smem_desc_sw128(base), bdesc0 = smem_desc_sw128(base + A_BYTES);
+    // A half waits for its own slot only, so that the halves' readers take turns at the FMA pipe.
     Ring rp, ap;
     bool ok = true;
     for (int t = first; t < p.tiles && ok; t += step) {
-      for (int kb = kb0; kb < kb1; ++kb, rp.next(RING), ap.next(N_ACC)) {
+      for (int kb = kb0; kb < kb1 && ok; ++kb, rp.next(RING)) {
         const uint32_t o = 8u * (uint32_t)rp.slot;
-        if (!mbar_wait_warp<true>(bar_tempty + 8u * ap.slot, ap.pass ^ 1u, abort_flag)) { ok = false; break; }
-        if (!mbar_wait_warp<true>(bar_full + o, rp.pass, abort_flag)) { ok = false; break; }
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint64_t so = (uint64_t)((uint32_t)(rp.slot * STAGE) >> 4);
-        const uint32_t d = tmem_base + (uint32_t)(ap.slot * BN);
-        if (leader) {
 #pragma unroll
-          for (int kk = 0; kk < BK / UMMA_K; ++kk)
-            mma_f8(d, adesc0 + so + (uint64_t)(kk * (UMMA_K >> 4)), bdesc0 + so + (uint64_t)(kk * (UMMA_K >> 4)), idesc, kk > 0 ? 1u : 0u);
-          mma_commit(bar_empty + o);
-          mma_commit(bar_tfull + 8u * ap.slot);
+        for (int h = 0; h < HALVES; ++h, ap.next(MAX_SLOTS)) {
+          ok = mbar_wait_warp<true>(bar_tempty + 8u * (uint32_t)ap.slot, ap.pass ^ 1u, abort_flag) &&
+               (h > 0 || mbar_wait_warp<true>(bar_full + o, rp.pass, abort_flag));
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t d = tmem_base + (uint32_t)(ap.slot * SLOT_COLS);
+          const uint64_t ad = adesc0 + so, bd = bdesc0 + so + (uint64_t)(h * 64 * BK >> 4);
+          if (leader) {
+#pragma unroll
+            for (int kk = 0; kk < BK / UMMA_K; ++kk)
+              mma_f8<PAIR>(d, ad + (uint64_t)(kk * (UMMA_K >> 4)), bd + (uint64_t)(kk * (UMMA_K >> 4)), idesc, kk > 0 ? 1u : 0u);
+            if (h == HALVES - 1) commit<PAIR>(bar_empty + o);
+            commit<PAIR>(bar_tfull + 8u * (uint32_t)ap.slot);
+          }
+          __syncwarp();
         }
-        __syncwarp();
       }
     }
   } else if (COLSCALE && warp == 2) {
-    // column scales of a k-block, for the accumulator of the same number; loaded one k-block ahead
-    Ring ap;
+    // ---- column scales of a tile's k-blocks ----
+    Ring cp;
     bool ok = true;
     for (int t = first; t < p.tiles && ok; t += step) {
       int mt, nt;
       tile_at(p, t, mt, nt);
-      float v[BN / 32];
-      auto load = [&](int kb) {
+      const float* at[BN / 32];
 #pragma unroll
-        for (int i = 0; i < BN / 32; ++i) v[i] = __ldg(p.g.w.scale + (long)min(nt * BN + i * 32 + lane, p.N - 1) * p.g.w.srs + (long)kb * p.g.w.scs);
-      };
-      load(kb0);
-      for (int kb = kb0; kb < kb1; ++kb, ap.next(N_ACC)) {
-        if (!mbar_wait_warp(bar_tempty + 8u * ap.slot, ap.pass ^ 1u, abort_flag)) { ok = false; break; }
+      for (int i = 0; i < BN / 32; ++i) at[i] = p.g.w.scale + (long)min(nt * BN + i * 32 + lane, p.N - 1) * p.g.w.srs;
+      for (int kb = kb0; kb < kb1; ++kb, cp.next(AHEAD)) {
+        if (!mbar_wait_warp(bar_cempty + 8u * (uint32_t)cp.slot, cp.pass ^ 1u, abort_flag)) { ok = false; break; }
 #pragma unroll
-        for (int i = 0; i < BN / 32; ++i) col_scales[ap.slot * BN + i * 32 + lane] = v[i];
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar_cols + 8u * ap.slot);
-        if (kb + 1 < kb1) load(kb + 1);
+        for (int i = 0; i < BN / 32; ++i) cp_async4(smem_u32(col_scales + cp.slot * BN + i * 32 + lane), at[i] + (long)kb * p.g.w.scs);
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_cfull + 8u * (uint32_t)cp.slot) : "memory");
       }
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp >= FIRST_EPI) {
-    if (exchanges_registers(BN)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(EPI_REGS));
+    // ---- sums in registers, output ----
+    if (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(EPI_REGS));
     const int q = warp & 3, half = (warp - FIRST_EPI) >> 2;
-    const uint32_t tmem_q = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * COLS);
+    // a pair's warps have whole slots (every second one), the others half the columns of every slot
+    const int slot_step = HALVES, col_in_slot = HALVES == 2 ? 0 : half * COLS;
+    const uint32_t tmem_q = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)col_in_slot;
     uint8_t* const my_staging = staging + (warp - FIRST_EPI) * STAGING;
-    Ring ap;
-    bool ok = true;
-    for (int t = first; t < p.tiles && ok; t += step) {
+    int slot = HALVES == 2 ? half : 0;
+    uint32_t pass = 0;
+    auto next_slot = [&]() { slot += slot_step; if (slot >= MAX_SLOTS) { slot -= MAX_SLOTS; pass ^= 1u; } };
+    const int k_count = kb1 - kb0;
+    auto place = [&](int t, int& row0, int& col0) {
       int mt, nt;
       tile_at(p, t, mt, nt);
-      const int row0 = mt * BM + q * 32, col0 = nt * BN + half * COLS;
-      const float* const sa = p.g.a.scale + (long)(min(row0 + lane, p.M - 1) / p.g.a.block_rows) * p.g.a.srs;
-      const float* const sw = p.g.w.scale + (COLSCALE ? 0L : (long)(min(col0, p.N - 1) / p.g.w.block_rows) * p.g.w.srs);
-      auto scale_of = [&](int kb) {
-        const float s = __ldg(sa + (long)kb * p.g.a.scs);
-        return COLSCALE ? s : __fmul_rn(s, __ldg(sw + (long)kb * p.g.w.scs));
-      };
+      row0 = mt * TILE_M + row_off + q * 32; col0 = nt * BN + half * COLS;
+    };
+    // The scales of AHEAD_REGS k-blocks are in flight to registers, across tiles; they are multiplied when they are used (a product here
+    // would wait for the loads).
+    constexpr int AHEAD_REGS = 4;
+    float a_next[AHEAD_REGS], w_next[AHEAD_REGS];
+    int ahead_t = first, ahead_k = 0;
+    const float *a_at = nullptr, *w_at = nullptr;
+    auto fetch = [&](int i) {
+      if (ahead_t >= p.tiles) return;
+      if (ahead_k == 0) {
+        int row0, col0;
+        place(ahead_t, row0, col0);
+        a_at = p.g.a.scale + (long)(min(row0 + lane, p.M - 1) / p.g.a.block_rows) * p.g.a.srs + (long)kb0 * p.g.a.scs;
+        w_at = p.g.w.scale + (long)(min(col0, p.N - 1) / p.g.w.block_rows) * p.g.w.srs + (long)kb0 * p.g.w.scs;
+      }
+      a_next[i] = __ldg(a_at);
+      if (!COLSCALE) w_next[i] = __ldg(w_at);
+      a_at += p.g.a.scs; w_at += p.g.w.scs;
+      if (++ahead_k == k_count) { ahead_k = 0; ahead_t += step; }
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD_REGS; ++i) { a_next[i] = 0.0f; w_next[i] = 1.0f; fetch(i); }
+    const uint32_t tempty_at = PAIR ? cluster_addr(bar_tempty, 0) : bar_tempty;
+    int col_slot = 0; uint32_t col_pass = 0;
+    bool ok = true;
+    constexpr int LD = COLS < 32 ? COLS : 32;                 // columns of a load; the next one is in flight during the sums
+    for (int t = first; t < p.tiles; t += step) {
       float2 acc[COLS / 2];
 #pragma unroll
       for (int i = 0; i < COLS / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
-      // scales two k-blocks ahead
-      float s1 = scale_of(kb0), s2 = kb0 + 1 < kb1 ? scale_of(kb0 + 1) : 0.0f;
-      for (int kb = kb0; kb < kb1; ++kb, ap.next(N_ACC)) {
-        const float2 s = f2(s1);
-        s1 = s2;
-        if (kb + 2 < kb1) s2 = scale_of(kb + 2);
-        if (COLSCALE && !mbar_wait_warp<true>(bar_cols + 8u * ap.slot, ap.pass, abort_flag)) { ok = false; break; }
-        if (!mbar_wait_warp<true>(bar_tfull + 8u * ap.slot, ap.pass, abort_flag)) { ok = false; break; }
+      for (int k = 0; k < k_count; ++k, next_slot()) {
+        const float a0 = a_next[0], w0 = w_next[0];
+#pragma unroll
+        for (int i = 0; i + 1 < AHEAD_REGS; ++i) { a_next[i] = a_next[i + 1]; w_next[i] = w_next[i + 1]; }
+        fetch(AHEAD_REGS - 1);
+        if (COLSCALE && !mbar_wait_warp<true>(bar_cfull + 8u * (uint32_t)col_slot, col_pass, abort_flag)) { ok = false; break; }
+        if (!mbar_wait_warp<true>(bar_tfull + 8u * (uint32_t)slot, pass, abort_flag)) { ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        constexpr int LD = COLS < 64 ? COLS : 64;             // columns in flight
-        const uint32_t d = tmem_q + (uint32_t)(ap.slot * BN);
-        const float4* const cs = reinterpret_cast<const float4*>(col_scales + ap.slot * BN + half * COLS);
+        const uint32_t d = tmem_q + (uint32_t)(slot * SLOT_COLS);
+        const float4* const cs = reinterpret_cast<const float4*>(col_scales + col_slot * BN + half * COLS);
+        float r[2][LD];
+        tmem_ld_rows(d, r[0]);
+        const float2 s = f2(COLSCALE ? a0 : __fmul_rn(a0, w0));
 #pragma unroll
         for (int c = 0; c < COLS; c += LD) {
-          float r[LD];
-#pragma unroll
-          for (int i = 0; i < LD; i += 16) tmem_ld16(d + (uint32_t)(c + i), r + i);
-          tmem_wait16(r);
-#pragma unroll
-          for (int i = 16; i < LD; i += 16) pass_through16(r + i);
-          if (!COLSCALE && c + LD == COLS) {                  // all is read: the tensor core may have the accumulator back
+          float (&v)[LD] = r[(c / LD) & 1];
+          tmem_wait(v);
+          if (c + LD < COLS) {
+            tmem_ld_rows(d + (uint32_t)(c + LD), r[(c / LD + 1) & 1]);
+          } else {                                            // all is read: the tensor core may have the slot back
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar_tempty + 8u * ap.slot);
+            if (lane == 0) {
+              if constexpr (PAIR) arrive_cluster(tempty_at + 8u * (uint32_t)slot);
+              else mbar_arrive(bar_tempty + 8u * (uint32_t)slot);
+            }
           }
 #pragma unroll
           for (int i = 0; i < LD; i += 4) {
-            float2 d0 = make_float2(r[i], r[i + 1]), d1 = make_float2(r[i + 2], r[i + 3]);
+            float2 d0 = make_float2(v[i], v[i + 1]), d1 = make_float2(v[i + 2], v[i + 3]);
             if (COLSCALE) {
               const float4 w = cs[(c + i) / 4];
               d0 = __fmul2_rn(d0, make_float2(w.x, w.y)); d1 = __fmul2_rn(d1, make_float2(w.z, w.w));
@@ -342,19 +447,21 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             acc[(c + i) / 2 + 1] = __ffma2_rn(d1, s, acc[(c + i) / 2 + 1]);
           }
         }
-        if (COLSCALE) {                                       // (the scales beside it have been read, too)
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        if (COLSCALE) {
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar_tempty + 8u * ap.slot);
+          if (lane == 0) mbar_arrive(bar_cempty + 8u * (uint32_t)col_slot);
+          if (++col_slot == AHEAD) { col_slot = 0; col_pass ^= 1u; }
         }
       }
       if (!ok) break;
+      int out_row, out_col;
+      place(t, out_row, out_col);
       if (p.split == 1) {
-        if (p.g.y_dtype == DT_F32) store_tile<float, COLS>(acc, my_staging, p, row0, col0, lane);
-        else if (p.g.y_dtype == DT_BF16) store_tile<__nv_bfloat16, COLS>(acc, my_staging, p, row0, col0, lane);
-        else store_tile<__half, COLS>(acc, my_staging, p, row0, col0, lane);
-      } else if (BN <= 128) {
-        // the part goes where the ring was: every stage has been multiplied when the last accumulator is complete
+        if (p.g.y_dtype == DT_F32) store_tile<float, COLS>(acc, my_staging, p, out_row, out_col, lane);
+        else if (p.g.y_dtype == DT_BF16) store_tile<__nv_bfloat16, COLS>(acc, my_staging, p, out_row, out_col, lane);
+        else store_tile<__half, COLS>(acc, my_staging, p, out_row, out_col, lane);
+      } else if (!PAIR) {
+        // the part goes where the ring was: every stage has been multiplied when the last slot is full
         const int r = q * 32 + lane;
 #pragma unroll
         for (int i = 0; i < COLS / 4; ++i) {
@@ -367,9 +474,9 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
   }
 
   __syncwarp();
-  if (p.split > 1) {
+  if (!PAIR && p.split > 1) {
     cluster_sync();
-    if (warp >= FIRST_EPI && BN <= 128 && first < p.tiles) {
+    if (warp >= FIRST_EPI) {
       int mt, nt;
       tile_at(p, first, mt, nt);
       const int e = tid - FIRST_EPI * 32;
@@ -382,22 +489,29 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   if (*abort_flag) {
-    // A wait ran out: the copies issued must have landed and the MMAs issued must have retired before the CTA may exit (bounded).
-    if (warp == 1 && elect_one()) mma_commit(bar_drain);
+    // A wait ran out: the copies issued must have landed and the MMAs issued must have retired before the CTA may exit (bounded).  The
+    // copies of a pair count on the first CTA's barriers, which that CTA waits for; if it did not give up, all have been multiplied.
+    const bool issuer = !PAIR || rank == 0;
+    if (issuer && warp == 1 && elect_one()) commit<PAIR>(bar_drain);
     __syncthreads();
     if (tid == 0) {
       atomicExch(p.g.status, 1);
       auto drain = [](uint32_t bar, uint32_t parity) {
         for (uint32_t it = 0; it < (1u << 20); ++it) if (mbar_try_wait(bar, parity)) return;
       };
-      for (uint32_t s = 0; s < (uint32_t)RING; ++s)
-        if (fills > s) drain(bar_full + 8u * s, (fills - 1u - s) / (uint32_t)RING & 1u);
-      drain(bar_drain, 0u);
+      if (issuer) {
+        for (uint32_t s = 0; s < (uint32_t)RING; ++s)
+          if (fills > s) drain(bar_full + 8u * s, (fills - 1u - s) / (uint32_t)RING & 1u);
+        drain(bar_drain, 0u);
+      }
     }
     __syncthreads();
   }
-  if (warp == 2)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)tmem_cols(BN)) : "memory");
+  if (PAIR) {
+    cluster_sync();                            // the MMAs read and write both CTAs' memory
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  }
+  if (warp == 2) tmem_dealloc<PAIR>(tmem_base, (uint32_t)tmem_cols(BN));
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------------
@@ -412,16 +526,17 @@ bool make_rows_map(CUtensorMap* m, const uint8_t* ptr, uint64_t rows, uint64_t c
 }
 
 struct Plan { int bn, split; };
-Plan pick_plan(long m_tiles, int N, int k_blocks, int sms) {
+Plan pick_plan(int M, int N, int k_blocks, int sms) {
   Plan best = {0, 0};
   double best_cost = 0.0;
   for (int bn = 32; bn <= 256; bn *= 2) {
-    const long tiles = m_tiles * ((N + bn - 1) / bn);
+    const int rows = paired(bn) ? 2 * BM : BM, ctas = paired(bn) ? 2 : 1;
+    const long tiles = (long)((M + rows - 1) / rows) * ((N + bn - 1) / bn);
     for (int split = 1; split <= MAX_SPLIT; split *= 2) {
-      if (split > 1 && (bn > 128 || split > k_blocks || tiles * split > sms)) break;
-      const long rounds = (tiles * split + sms - 1) / sms;
+      if (split > 1 && (paired(bn) || split > k_blocks || tiles * split > sms)) break;
+      const long rounds = (tiles * split + sms / ctas - 1) / (sms / ctas);
       const int blocks = (k_blocks + split - 1) / split;
-      const double block = bn == 256 ? 0.31 : bn == 128 ? 0.17 : 0.13;
+      const double block = bn == 256 ? 0.31 : bn == 128 ? 0.27 : 0.18;
       const double cost = rounds * (blocks * block + (split > 1 ? 1.5 : 0.0) + 0.004 * bn) + 2.0;
       if (!best.bn || cost <= best_cost) { best = {bn, split}; best_cost = cost; }
     }
@@ -429,37 +544,54 @@ Plan pick_plan(long m_tiles, int N, int k_blocks, int sms) {
   return best;
 }
 
+// Per device, once: opt in to the shared memory, check that the register shares fit into what the block is launched with, and count
+// the pairs that run at once (a GPC with an odd number of SMs leaves one over).  Returns 0 on failure.
 template <int BN, bool COLSCALE>
-bool set_up() {
-  // per device: opt in to the shared memory, and check that the register shares fit into what the block is launched with
-  static std::atomic<uint64_t> done{0};
+int set_up(int sms) {
+  static_assert(smem_total(BN, COLSCALE) + 1024 <= 227 * 1024, "shared memory");
+  static std::atomic<int> at_once[64];
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev > 63) return false;
-  if (done.load(std::memory_order_acquire) >> dev & 1) return true;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev > 63) return 0;
+  int n = at_once[dev].load(std::memory_order_relaxed);
+  if (n) return n;
   cudaFuncAttributes at;
-  if (cudaFuncSetAttribute(k_fp8_gemm<BN, COLSCALE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_total(BN) + 1024) != cudaSuccess ||
-      cudaFuncGetAttributes(&at, k_fp8_gemm<BN, COLSCALE>) != cudaSuccess)
-    return false;
-  if (exchanges_registers(BN) && FIRST_EPI * SIDE_REGS + EPI_WARPS * EPI_REGS > (FIRST_EPI + EPI_WARPS) * at.numRegs) return false;
-  done.fetch_or(1ull << dev, std::memory_order_release);
-  return true;
+  const auto kernel = k_fp8_gemm<BN, COLSCALE>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_total(BN, COLSCALE) + 1024) != cudaSuccess ||
+      cudaFuncGetAttributes(&at, kernel) != cudaSuccess)
+    return 0;
+  n = sms;
+  if (paired(BN)) {
+    if (FIRST_EPI * SIDE_REGS + EPI_WARPS * EPI_REGS > (FIRST_EPI + EPI_WARPS) * at.numRegs) return 0;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2; attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(sms / 2 * 2)); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = smem_total(BN, COLSCALE) + 1024;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) return 0;
+  }
+  at_once[dev].store(n, std::memory_order_relaxed);
+  return n;
 }
 
 template <int BN, bool COLSCALE>
 bool launch_as(const Params& p, cudaStream_t st, int sms) {
-  static_assert(smem_total(BN) + 1024 <= 227 * 1024, "shared memory");
-  if (!set_up<BN, COLSCALE>()) return false;
+  const int at_once = set_up<BN, COLSCALE>(sms);
+  if (!at_once) return false;
   CUtensorMap mA, mW;
-  if (!make_rows_map(&mA, p.g.a.codes, p.M, p.g.K, p.g.a.stride, BM) || !make_rows_map(&mW, p.g.w.codes, p.N, p.g.K, p.g.w.stride, BN)) return false;
+  if (!make_rows_map(&mA, p.g.a.codes, p.M, p.g.K, p.g.a.stride, BM) ||
+      !make_rows_map(&mW, p.g.w.codes, p.N, p.g.K, p.g.w.stride, paired(BN) ? 64 : BN))
+    return false;
+  const int cluster = paired(BN) ? 2 : p.split;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = p.split; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.gridDim = dim3((unsigned)(p.split > 1 ? p.tiles * p.split : p.tiles < sms ? p.tiles : sms));
-  cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = smem_total(BN) + 1024; cfg.stream = st;
-  cfg.attrs = attr; cfg.numAttrs = p.split > 1 ? 2 : 1;
+  attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)(cluster * (p.split > 1 || p.tiles < at_once ? p.tiles : at_once)));
+  cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = smem_total(BN, COLSCALE) + 1024; cfg.stream = st;
+  cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
   cudaLaunchKernelEx(&cfg, k_fp8_gemm<BN, COLSCALE>, mA, mW, p);
   ++g_launches;
   return true;
@@ -471,9 +603,9 @@ bool launch_fp8_matmul(const Fp8MatmulArgs& g, cudaStream_t st) {
   Params p;
   p.g = g; p.M = (int)g.a.rows; p.N = (int)g.w.rows;
   p.k_blocks = (int)((g.K + BK - 1) / BK);
-  p.m_tiles = (p.M + BM - 1) / BM;
   const int sms = sm_count();
-  const Plan plan = pick_plan(p.m_tiles, p.N, p.k_blocks, sms);
+  const Plan plan = pick_plan(p.M, p.N, p.k_blocks, sms);
+  p.m_tiles = (p.M + (paired(plan.bn) ? 2 * BM : BM) - 1) / (paired(plan.bn) ? 2 * BM : BM);
   p.n_tiles = (p.N + plan.bn - 1) / plan.bn;
   if ((long)p.m_tiles * p.n_tiles >= (1L << 31) - sms) return false;
   p.tiles = p.m_tiles * p.n_tiles; p.split = plan.split;
