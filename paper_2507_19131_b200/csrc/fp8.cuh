@@ -75,8 +75,10 @@ __device__ __forceinline__ void block_scale(float amax, bool pow2, float& scale,
     scale = __uint_as_float((uint32_t)e << 23);
     inv = __uint_as_float((uint32_t)(254 - e) << 23);
   } else {
-    scale = fmaxf(__fdiv_rn(a, 448.0f), 1.17549435e-38f);
-    inv = __fdiv_rn(1.0f, scale);
+    // a / 448, correctly rounded (Markstein): the product with the rounded reciprocal, corrected by its exact remainder
+    const float r = 2.23214296e-3f, t = __fmul_rn(a, r);
+    scale = fmaxf(__fmaf_rn(__fmaf_rn(-448.0f, t, a), r, t), 1.17549435e-38f);
+    inv = __frcp_rn(scale);
   }
   if (!(a <= 3.402823466e38f)) scale = inv = __uint_as_float(0x7fc00000u);
 }
@@ -86,6 +88,12 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
   const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
   const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
   return lo | (hi << 16);
+}
+__device__ __forceinline__ uint2 codes8(const float2 (&f)[4], float inv) {
+  float2 t[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t[i] = __fmul2_rn(f[i], make_float2(inv, inv));
+  return make_uint2(codes4(t[0].x, t[0].y, t[1].x, t[1].y), codes4(t[2].x, t[2].y, t[3].x, t[3].y));
 }
 __device__ __forceinline__ uint2 codes8(const float (&f)[8], float inv) {
   return make_uint2(codes4(__fmul_rn(f[0], inv), __fmul_rn(f[1], inv), __fmul_rn(f[2], inv), __fmul_rn(f[3], inv)),

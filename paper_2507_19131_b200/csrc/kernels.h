@@ -192,9 +192,9 @@ struct ResNormGradArgs {
   float* workspace;
 };
 constexpr int NORM_MAX_DIM = 16384;
-void launch_residual_norm(const ResNormArgs& a, cudaStream_t st);
+void launch_residual_norm(const ResNormArgs& a, int* status, cudaStream_t st);
 size_t residual_norm_backward_floats(long rows, int dim, bool gate_per_sequence);   // of the workspace
-void launch_residual_norm_backward(const ResNormArgs& a, const ResNormGradArgs& g, cudaStream_t st);
+void launch_residual_norm_backward(const ResNormArgs& a, const ResNormGradArgs& g, int* status, cudaStream_t st);
 
 // ---- preparation -----------------------------------------------------------------------------------
 void launch_prepare_linear(const int8_t* w, const float* sw, int N, int K, float sa, int za, int bits, float* mult,

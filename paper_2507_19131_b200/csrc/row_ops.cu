@@ -179,7 +179,7 @@ mixaq_status mixaq_residual_norm_forward(mixaq_ctx* ctx, const mixaq_residual_no
   g_launches = 0;
   try {
     ProfScope scope(ctx, PC_RES_NORM, st);
-    launch_residual_norm(a, st);
+    launch_residual_norm(a, ctx->d_status, st);
   } catch (...) { return fail(ctx, MIXAQ_INTERNAL, "residual_norm_forward: out of host memory"); }
   ctx->launches = g_launches;
   return check_cuda(ctx, "residual_norm_forward");
@@ -233,7 +233,7 @@ mixaq_status mixaq_residual_norm_backward(mixaq_ctx* ctx, const mixaq_residual_n
   a.workspace = static_cast<float*>(workspace);
   try {
     ProfScope scope(ctx, PC_RES_NORM, st);
-    launch_residual_norm_backward(norm_args(*p), a, st);
+    launch_residual_norm_backward(norm_args(*p), a, ctx->d_status, st);
   } catch (...) { return fail(ctx, MIXAQ_INTERNAL, "residual_norm_backward: out of host memory"); }
   ctx->launches = g_launches;
   return check_cuda(ctx, "residual_norm_backward");
