@@ -30,35 +30,16 @@ template <class T> __device__ __forceinline__ void load_some8(const T* p, int n,
 #pragma unroll
   for (int i = 0; i < 8; ++i) r.v[i] = i < n ? __ldg(p + i) : from_f32<T>(0.0f);
 }
-// loads of memory that the kernel itself may write later (rows updated in place)
-template <class T> __device__ __forceinline__ void load_row8(const T* p, bool vec, int n, Vec8<T>& r) {
-  if (vec && n >= 8) {
-    uint4* d = reinterpret_cast<uint4*>(&r);
+// a load of memory that the kernel itself may write later (rows updated in place); p 16-byte aligned
+template <class T> __device__ __forceinline__ void load_row8(const T* p, Vec8<T>& r) {
+  uint4* d = reinterpret_cast<uint4*>(&r);
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(Vec8<T>) / 16; ++i) d[i] = reinterpret_cast<const uint4*>(p)[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r.v[i] = i < n ? p[i] : from_f32<T>(0.0f);
-  }
+  for (int i = 0; i < (int)sizeof(Vec8<T>) / 16; ++i) d[i] = reinterpret_cast<const uint4*>(p)[i];
 }
 template <class T> __device__ __forceinline__ void unpack8(const Vec8<T>& r, float (&f)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = to_f32(r.v[i]);
 }
-template <class T> __device__ __forceinline__ void store8(T* p, const float (&f)[8], bool vec, int n) {
-  Vec8<T> r;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) r.v[i] = from_f32<T>(f[i]);
-  if (vec) {
-    const uint4* s = reinterpret_cast<const uint4*>(&r);
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(Vec8<T>) / 16; ++i) reinterpret_cast<uint4*>(p)[i] = s[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) if (i < n) p[i] = r.v[i];
-  }
-}
-
 // max(|a|, |b|), no number if either is none (the sign of the result means nothing)
 __device__ __forceinline__ float max_abs(float a, float b) {
   float r;

@@ -45,7 +45,7 @@ __device__ __forceinline__ F8 load_cols(const T* row, int i, int l, int dim) {
   if constexpr (VEC) {
     if (present<TPR, VEC>(i, 0, l, dim)) {
       Vec8<T> r;
-      load_row8(row + column<TPR, VEC>(i, 0, l), true, 8, r);
+      load_row8(row + column<TPR, VEC>(i, 0, l), r);
 #pragma unroll
       for (int j = 0; j < 4; ++j) f.v[j] = unpack2(r.v + 2 * j);
     }
@@ -237,7 +237,7 @@ inline bool rows_aligned(const void* p, long stride, size_t size) {
 }
 // Stages of `stage_bytes` for the workers of a CTA, of which `ctas` at most share an SM: fewer CTAs where not even two stages fit, and
 // no ring (0) where a single CTA has no room for them.
-constexpr int RING_BYTES_PER_SM = 132 * 1024;
+constexpr int RING_BYTES_PER_SM = 150 * 1024;
 inline int ring_stages(long stage_bytes, int workers, int& ctas) {
   for (; ctas > 0; --ctas) {
     const long n = RING_BYTES_PER_SM / ctas / workers / stage_bytes;
