@@ -676,7 +676,7 @@ def fp8_quantize(ctx: Context, x: torch.Tensor, block_rows: int = 1, transpose: 
         out = Fp8Matrix.empty(r, c, block_rows, x.device)
     elif out.block_rows != block_rows:
         raise MixaqError(-1, "out has other blocks")
-    st = _lib.mixaq_fp8_quantize(ctx.h, x.data_ptr(), _DTYPES[x.dtype], rows, cols, ld, transpose, pow2, out.pack(ctx, "out"), _stream())
+    st = lib().mixaq_fp8_quantize(ctx.h, x.data_ptr(), _DTYPES[x.dtype], rows, cols, ld, transpose, pow2, out.pack(ctx, "out"), _stream())
     if st:
         ctx.check(st, "fp8_quantize")
     return out
@@ -695,7 +695,7 @@ def fp8_matmul(ctx: Context, a: Fp8Matrix, w: Fp8Matrix, bias: Optional[torch.Te
     else:
         ld = _ld(ctx, y, m, n, "y")
         _need(y.dtype in _DTYPES, f"y: float32, bfloat16 or float16 is needed, got {y.dtype}")
-    st = _lib.mixaq_fp8_matmul(ctx.h, pa, pw, _vector(ctx, bias, n, "bias"), y.data_ptr(), _DTYPES[y.dtype], ld, _stream())
+    st = lib().mixaq_fp8_matmul(ctx.h, pa, pw, _vector(ctx, bias, n, "bias"), y.data_ptr(), _DTYPES[y.dtype], ld, _stream())
     if st:
         ctx.check(st, "fp8_matmul")
     return y
@@ -768,7 +768,7 @@ def residual_norm_forward(ctx: Context, x: torch.Tensor, y: Optional[torch.Tenso
     g_at, g_dtype, g_ld, per, _ = _gate_fields(ctx, gate, rows_per_gate, rows, dim, y_dtype)
     p = _NORM_PARAMS.pack(rows, dim, _DTYPES[x.dtype], _DTYPES[y_dtype], g_dtype, x.data_ptr(), x_ld, y_at, y_ld, g_at, g_ld, per, scale,
                           *_norm_fields(ctx, post, dim, "post"), *_norm_fields(ctx, pre, dim, "pre"), out_at, out_ld, h_at, h_ld, pow2)
-    st = _lib.mixaq_residual_norm_forward(ctx.h, p, packed, _stream())
+    st = lib().mixaq_residual_norm_forward(ctx.h, p, packed, _stream())
     if st:
         ctx.check(st, "residual_norm_forward")
     return SimpleNamespace(x=new_x, h=h)
@@ -813,11 +813,11 @@ def residual_norm_backward(ctx: Context, x: Optional[torch.Tensor], y: Optional[
     at = [getattr(out, name).data_ptr() if getattr(out, name) is not None else 0 for name in ("dpost_gamma", "dpost_beta", "dpre_gamma", "dpre_beta")]
     g = _NORM_GRADS.pack(*place(dx_out, x_dtype, "dx_out"), *place(dh, y_dtype, "dh"), out.dx.data_ptr(), dim,
                          out.dy.data_ptr() if y is not None else 0, dim, out.dgate.data_ptr() if gate is not None else 0, dim, *at)
-    need = _lib.mixaq_residual_norm_backward_workspace_bytes(p)
+    need = lib().mixaq_residual_norm_backward_workspace_bytes(p)
     if workspace is None:
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
     _need(workspace.device == ctx.device and workspace.is_contiguous(), f"workspace: a contiguous tensor on {ctx.device} is needed")
-    st = _lib.mixaq_residual_norm_backward(ctx.h, p, g, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream())
+    st = lib().mixaq_residual_norm_backward(ctx.h, p, g, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream())
     if st:
         ctx.check(st, "residual_norm_backward")
     return out

@@ -64,7 +64,7 @@ mixaq_status check_residual_norm(mixaq_ctx* ctx, const mixaq_residual_norm_param
   if (!dtype_ok(p->x_dtype) || !dtype_ok(p->y_dtype)) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: unknown dtype");
   if (p->x_dtype != MIXAQ_F32 && p->x_dtype != p->y_dtype) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: a 16-bit x needs y of its own type");
   if (!norm_ok(p->post) || !norm_ok(p->pre)) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: norm kind unknown, eps not positive, or gamma or beta not 4-byte aligned");
-  if (!p->y && (p->gate || p->post.kind != MIXAQ_NORM_NONE)) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: gate or post norm without y");
+  if (p->rows > 0 && !p->y && (p->gate || p->post.kind != MIXAQ_NORM_NONE)) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: gate or post norm without y");
   if (p->gate) {
     if (p->gate_dtype != p->y_dtype && p->gate_dtype != MIXAQ_F32) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: gate_dtype must be y_dtype or MIXAQ_F32");
     if (p->rows_per_gate < 1) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: rows_per_gate must be at least 1");
@@ -153,9 +153,9 @@ mixaq_status mixaq_residual_norm_forward(mixaq_ctx* ctx, const mixaq_residual_no
   ctx->launches = 0;
   if (mixaq_status s = check_residual_norm(ctx, p)) return s;
   const bool pre = p->pre.kind != MIXAQ_NORM_NONE;
-  if (pre ? !p->h == !h_fp8 : p->h || h_fp8) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: a pre norm needs h or h_fp8, one of them; none takes neither");
-  if (!pre && !p->y) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: neither y nor a pre norm");
-  if (!p->y && p->x_out) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: x_out without y");
+  if (pre ? (p->h && h_fp8) || (p->rows > 0 && !p->h && !h_fp8) : p->h || h_fp8) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: a pre norm needs h or h_fp8, one of them; none takes neither");
+  if (p->rows > 0 && !pre && !p->y) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: neither y nor a pre norm");
+  if (p->rows > 0 && !p->y && p->x_out) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: x_out without y");
   if (h_fp8) {
     if (h_fp8->rows != p->rows || h_fp8->cols != p->dim || h_fp8->block_rows != 1) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm: h_fp8 has another shape than x, or block_rows other than 1");
     if (mixaq_status s = check_matrix(ctx, h_fp8, true)) return s;
@@ -198,7 +198,7 @@ mixaq_status mixaq_residual_norm_backward(mixaq_ctx* ctx, const mixaq_residual_n
   if (!g) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm_backward: grads are NULL");
   const bool pre = p->pre.kind != MIXAQ_NORM_NONE, post = p->post.kind != MIXAQ_NORM_NONE;
   float* const vec[4] = {g->dpost_gamma, g->dpost_beta, g->dpre_gamma, g->dpre_beta};
-  if ((!pre && (g->dh || vec[2] || vec[3])) || (!post && (vec[0] || vec[1])) || (!p->y && g->dy) || (!p->gate && g->dgate))
+  if ((!pre && (g->dh || vec[2] || vec[3])) || (!post && (vec[0] || vec[1])) || (p->rows > 0 && ((!p->y && g->dy) || (!p->gate && g->dgate))))
     return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm_backward: a gradient of something that is missing");
   for (const float* v : vec) if (!aligned_to(v, 4)) return fail(ctx, MIXAQ_INVALID_ARG, "residual_norm_backward: parameter gradients must be 4-byte aligned");
   if (p->rows > 0) {
