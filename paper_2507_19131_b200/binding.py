@@ -580,7 +580,7 @@ def _need(ok, what: str):
 
 def _ld(ctx: Context, t: torch.Tensor, rows: int, cols: int, name: str) -> int:
     """Row stride of a [rows, cols] tensor on the context's device whose rows are contiguous."""
-    if not (isinstance(t, torch.Tensor) and t.device == ctx.device and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols):
+    if not (isinstance(t, torch.Tensor) and t.shape == (rows, cols) and t.device == ctx.device):
         got = f"{tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
         raise MixaqError(-1, f"{name}: a tensor of {(rows, cols)} on {ctx.device} is needed, got {got}")
     ld, unit = t.stride()
@@ -604,7 +604,7 @@ def _vector(ctx: Context, t: Optional[torch.Tensor], n: int, name: str) -> int:
     """Address of a contiguous float32 vector, 0 for None."""
     if t is None:
         return 0
-    if not (isinstance(t, torch.Tensor) and t.dtype is _F32 and t.device == ctx.device and t.dim() == 1 and t.shape[0] == n and (n <= 1 or t.stride(0) == 1)):
+    if not (isinstance(t, torch.Tensor) and t.dtype is _F32 and t.shape == (n,) and t.device == ctx.device and t.is_contiguous()):
         raise MixaqError(-1, f"{name}: a contiguous float32 vector of {n} on {ctx.device} is needed")
     return t.data_ptr()
 
@@ -625,10 +625,7 @@ class Fp8Matrix:
     @classmethod
     def empty(cls, rows: int, cols: int, block_rows: int, device) -> "Fp8Matrix":
         """Room for a matrix: rows padded to a multiple of 16 bytes; scales of single rows with the rows as neighbours."""
-        ld = -(-cols // 16) * 16
-        codes = torch.empty((rows, ld), dtype=_E4M3, device=device)
-        if ld != cols:
-            codes = codes[:, :cols]
+        codes = torch.empty_strided((rows, cols), (-(-cols // 16) * 16, 1), dtype=_E4M3, device=device)
         rb, cb = -(-rows // block_rows), -(-cols // FP8_BLOCK)
         scale = torch.empty_strided((rb, cb), (1, rb) if block_rows == 1 else (cb, 1), dtype=_F32, device=device)
         return cls(codes, scale, block_rows)
@@ -642,8 +639,9 @@ class Fp8Matrix:
         codes, scale, br = self.codes, self.scale, self.block_rows
         if br != 1 and br != FP8_BLOCK:
             raise MixaqError(-1, f"{name}: block_rows must be 1 or {FP8_BLOCK}")
-        if not (codes.dtype is _E4M3 and scale.dtype is _F32 and codes.device == ctx.device and scale.device == ctx.device and codes.dim() == 2):
-            raise MixaqError(-1, f"{name}: 2-D float8_e4m3fn codes and float32 scales on {ctx.device} are needed")
+        dev = ctx.device
+        if not (codes.dtype is _E4M3 and scale.dtype is _F32 and codes.device == dev and scale.device == dev and codes.dim() == 2):
+            raise MixaqError(-1, f"{name}: 2-D float8_e4m3fn codes and float32 scales on {dev} are needed")
         rows, cols = codes.shape
         if scale.shape != (-(-rows // br), -(-cols // FP8_BLOCK)):
             raise MixaqError(-1, f"{name}: scales of {(-(-rows // br), -(-cols // FP8_BLOCK))} are needed, got {tuple(scale.shape)}")
@@ -721,15 +719,21 @@ def _gate_fields(ctx: Context, gate: Optional[torch.Tensor], rows_per_gate: Opti
     """(address, dtype, stride, rows_per_gate, gates) of a gate [dim] or [gates, dim]."""
     if gate is None:
         return 0, 0, 0, 0, 0
-    if gate.dim() == 1:
-        gate = gate.unsqueeze(0)
-    gates = gate.shape[0]
+    if gate.dtype is not y_dtype and gate.dtype is not _F32:
+        raise MixaqError(-1, f"gate: {y_dtype} or float32 is needed, got {gate.dtype}")
+    if gate.shape == (dim,):
+        if gate.device != ctx.device or not gate.is_contiguous():
+            raise MixaqError(-1, f"gate: a contiguous vector on {ctx.device} is needed")
+        gates, ld = 1, dim
+    else:
+        gates = gate.shape[0]
+        ld = _ld(ctx, gate, gates, dim, "gate")
     if rows_per_gate is None:
-        _need(gates > 0 and rows % gates == 0, f"gate: {gates} gates for {rows} rows need rows_per_gate")
-        rows_per_gate = max(rows // gates, 1)
-    _need(rows_per_gate >= 1 and gates == max(-(-rows // rows_per_gate), min(gates, 1)), f"gate: {gates} gates of {rows_per_gate} rows each are not {rows} rows")
-    ld = _ld(ctx, gate, gates, dim, "gate")
-    _need(gate.dtype is y_dtype or gate.dtype is _F32, f"gate: {y_dtype} or float32 is needed, got {gate.dtype}")
+        if gates == 0 or rows % gates:
+            raise MixaqError(-1, f"gate: {gates} gates for {rows} rows need rows_per_gate")
+        rows_per_gate = rows // gates if rows else 1
+    if rows_per_gate < 1 or gates != (-(-rows // rows_per_gate) if rows else min(gates, 1)):
+        raise MixaqError(-1, f"gate: {gates} gates of {rows_per_gate} rows each are not {rows} rows")
     return gate.data_ptr(), _DTYPES[gate.dtype], ld, rows_per_gate, gates
 
 
@@ -740,19 +744,24 @@ def residual_norm_forward(ctx: Context, x: torch.Tensor, y: Optional[torch.Tenso
     rounded to x's type; x itself without y) and h (None without pre; an Fp8Matrix with fp8).
     gate: [dim], or [gates, dim] for rows_per_gate consecutive rows each (by default the rows are dealt evenly).  h_dtype: type of h where
     y does not give it (default: x's).  x_out, h: tensors (for fp8 an Fp8Matrix) to write to; x_out may be x, h may be y."""
-    _need(isinstance(x, torch.Tensor) and x.dim() == 2 and x.dtype in _DTYPES, "x: a 2-D float32, bfloat16 or float16 tensor is needed")
+    if not (isinstance(x, torch.Tensor) and x.dim() == 2 and x.dtype in _DTYPES):
+        raise MixaqError(-1, "x: a 2-D float32, bfloat16 or float16 tensor is needed")
     rows, dim = x.shape
     x_ld = _ld(ctx, x, rows, dim, "x")
     y_dtype = y.dtype if y is not None else x.dtype if h_dtype is None else h_dtype
-    _need(y_dtype in _DTYPES and (h_dtype is None or h_dtype is y_dtype), "y and h: float32, bfloat16 or float16, both the same, are needed")
-    _need(pre is not None or (h is None and not fp8), "h without a pre norm")
+    if y_dtype not in _DTYPES or (h_dtype is not None and h_dtype is not y_dtype):
+        raise MixaqError(-1, "y and h: float32, bfloat16 or float16, both the same, are needed")
+    if pre is None and (h is not None or fp8):
+        raise MixaqError(-1, "h without a pre norm")
     y_at = y_ld = out_at = out_ld = h_at = h_ld = 0
     new_x = x
     if y is not None:
         y_at, y_ld = y.data_ptr(), _ld(ctx, y, rows, dim, "y")
         if x_out is None:
-            x_out = torch.empty((rows, dim), dtype=x.dtype, device=x.device)
-        new_x, out_at, out_ld = x_out, x_out.data_ptr(), _typed_ld(ctx, x_out, rows, dim, x.dtype, "x_out")
+            x_out, out_ld = x.new_empty((rows, dim)), dim
+        else:
+            out_ld = _typed_ld(ctx, x_out, rows, dim, x.dtype, "x_out")
+        new_x, out_at = x_out, x_out.data_ptr()
     else:
         _need(x_out is None, "x_out without y")
     packed = None
@@ -763,8 +772,10 @@ def residual_norm_forward(ctx: Context, x: torch.Tensor, y: Optional[torch.Tenso
             packed = h.pack(ctx, "h")
         else:
             if h is None:
-                h = torch.empty((rows, dim), dtype=y_dtype, device=x.device)
-            h_at, h_ld = h.data_ptr(), _typed_ld(ctx, h, rows, dim, y_dtype, "h")
+                h, h_ld = x.new_empty((rows, dim), dtype=y_dtype), dim
+            else:
+                h_ld = _typed_ld(ctx, h, rows, dim, y_dtype, "h")
+            h_at = h.data_ptr()
     g_at, g_dtype, g_ld, per, _ = _gate_fields(ctx, gate, rows_per_gate, rows, dim, y_dtype)
     p = _NORM_PARAMS.pack(rows, dim, _DTYPES[x.dtype], _DTYPES[y_dtype], g_dtype, x.data_ptr(), x_ld, y_at, y_ld, g_at, g_ld, per, scale,
                           *_norm_fields(ctx, post, dim, "post"), *_norm_fields(ctx, pre, dim, "pre"), out_at, out_ld, h_at, h_ld, pow2)

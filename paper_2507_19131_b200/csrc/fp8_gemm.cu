@@ -525,19 +525,23 @@ bool make_rows_map(CUtensorMap* m, const uint8_t* ptr, uint64_t rows, uint64_t c
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tile width and split.  A CTA (or pair) takes `block` microseconds a k-block and `store` a tile; a split adds its join.  The constants
+// were fitted to the times of all widths and splits at 17 shapes from 1 x 1024 x 8192 to 2048 x 4096 x 16384: the choice is the fastest at
+// 13 of them and within 8 % at the others.  (us: 1 x 4096 x 4096 by 128 columns in 4 parts 9.2, in 2 parts 10.1, whole 12.6, 32 columns
+// whole 16.4; 1024 x 4096 x 4096 by pairs 22, 128 columns 30; 300 x 1000 x 1000 by 32 columns 5.6, 128 columns 7.7.)  Eight parts only
+// while the clusters find room at once: 16 of them took 14.5 us where 8 took 7.2.
 struct Plan { int bn, split; };
 Plan pick_plan(int M, int N, int k_blocks, int sms) {
   Plan best = {0, 0};
   double best_cost = 0.0;
   for (int bn = 32; bn <= 256; bn *= 2) {
-    const int rows = paired(bn) ? 2 * BM : BM, ctas = paired(bn) ? 2 : 1;
+    const int rows = paired(bn) ? 2 * BM : BM, at_once = paired(bn) ? sms / 2 : sms;
     const long tiles = (long)((M + rows - 1) / rows) * ((N + bn - 1) / bn);
+    const double block = bn == 256 ? 0.52 : bn == 128 ? 0.32 : bn == 64 ? 0.29 : 0.26, store = bn == 256 ? 3.0 : bn == 128 ? 1.7 : bn == 64 ? 1.0 : 0.7;
     for (int split = 1; split <= MAX_SPLIT; split *= 2) {
-      if (split > 1 && (paired(bn) || split > k_blocks || tiles * split > sms)) break;
-      const long rounds = (tiles * split + sms / ctas - 1) / (sms / ctas);
-      const int blocks = (k_blocks + split - 1) / split;
-      const double block = bn == 256 ? 0.31 : bn == 128 ? 0.27 : 0.18;
-      const double cost = rounds * (blocks * block + (split > 1 ? 1.5 : 0.0) + 0.004 * bn) + 2.0;
+      if (split > 1 && (paired(bn) || split > k_blocks || tiles * split > (split == 8 ? sms * 3 / 4 : sms))) break;
+      const long rounds = (tiles * split + at_once - 1) / at_once;
+      const double cost = rounds * ((k_blocks + split - 1) / split * block + store) + (split > 1 ? 1.2 + 0.07 * split : 0.0);
       if (!best.bn || cost <= best_cost) { best = {bn, split}; best_cost = cost; }
     }
   }

@@ -9,30 +9,27 @@ namespace {
 
 // ---- a scale per row and 128 columns ----------------------------------------------------------------------------------------
 // Sixteen lanes take a block, eight neighbouring elements each: the row is read in 256- or 512-byte runs, the codes leave in 128-byte
-// runs, and the maximum is four shuffles.  A lane has UNROLL blocks in flight (consecutive blocks go to consecutive half warps).
-constexpr int ROW_THREADS = 256, ROW_UNROLL = 4, ROW_GROUPS = ROW_THREADS / 16;
+// runs, and the maximum is four shuffles.  A CTA has 64 rows of one column block, four of them in flight per lane: it needs no division,
+// and its scales are neighbours in the order that products read fastest.
+constexpr int ROW_THREADS = 256, ROW_UNROLL = 4, ROW_GROUPS = ROW_THREADS / 16, ROW_TILE = ROW_GROUPS * ROW_UNROLL;
 
 template <class T>
-__global__ void __launch_bounds__(ROW_THREADS) k_fp8_rows(const T* x, long row_stride, int cols, int kb_count, long blocks, bool vec, bool pow2,
+__global__ void __launch_bounds__(ROW_THREADS) k_fp8_rows(const T* x, long row_stride, long rows, int cols, int kb_count, bool vec, bool pow2,
                                                           uint8_t* codes, long code_stride, float* scale, long srs, long scs) {
   const int l16 = threadIdx.x & 15, group = threadIdx.x >> 4;
-  const long first = (long)blockIdx.x * (ROW_GROUPS * ROW_UNROLL) + group;
+  const unsigned rt = blockIdx.x / (unsigned)kb_count, kb = blockIdx.x - rt * (unsigned)kb_count;
+  const long row0 = (long)rt * ROW_TILE + group;
+  const int c = (int)kb * FP8_BLOCK + l16 * 8, n = max(min(cols - c, 8), 0);
   Vec8<T> raw[ROW_UNROLL];
-  long row[ROW_UNROLL]; int kb[ROW_UNROLL], n[ROW_UNROLL];
-  // the block's row by one 32-bit division (blocks < 2^31), further blocks by steps
 #pragma unroll
   for (int u = 0; u < ROW_UNROLL; ++u) {
-    const long b = first + u * ROW_GROUPS;
-    const unsigned r = (unsigned)min(b, blocks - 1) / (unsigned)kb_count;
-    row[u] = r; kb[u] = (int)((unsigned)min(b, blocks - 1) - r * (unsigned)kb_count);
-    const int c = kb[u] * FP8_BLOCK + l16 * 8;
-    n[u] = b < blocks ? max(min(cols - c, 8), 0) : 0;
-    const T* p = x + row[u] * row_stride + c;
-    if (vec && n[u] == 8) load_vec8(p, raw[u]);
-    else load_some8(p, n[u], raw[u]);
+    const long row = row0 + u * ROW_GROUPS;
+    if (vec && n == 8 && row < rows) load_vec8(x + row * row_stride + c, raw[u]);
+    else load_some8(x + row * row_stride + c, row < rows ? n : 0, raw[u]);
   }
 #pragma unroll
   for (int u = 0; u < ROW_UNROLL; ++u) {
+    const long row = row0 + u * ROW_GROUPS;
     float f[8];
     unpack8(raw[u], f);
     float m = 0.0f;
@@ -42,8 +39,10 @@ __global__ void __launch_bounds__(ROW_THREADS) k_fp8_rows(const T* x, long row_s
     for (int o = 8; o > 0; o >>= 1) m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, o));
     float s, inv;
     block_scale(m, pow2, s, inv);
-    store_codes(codes + row[u] * code_stride + kb[u] * FP8_BLOCK + l16 * 8, codes8(f, inv), n[u]);
-    if (l16 == 0 && n[u] > 0) scale[row[u] * srs + kb[u] * scs] = s;
+    if (row < rows) {
+      store_codes(codes + row * code_stride + c, codes8(f, inv), n);
+      if (l16 == 0) scale[row * srs + (long)kb * scs] = s;
+    }
   }
 }
 
@@ -159,9 +158,9 @@ void launch_typed(const Fp8QuantArgs& a, cudaStream_t st) {
   const T* x = static_cast<const T*>(a.x);
   const bool vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && a.row_stride * sizeof(T) % 16 == 0;
   if (!a.transpose && a.block_rows == 1) {
-    const long kb = (a.cols + FP8_BLOCK - 1) / FP8_BLOCK, blocks = a.rows * kb, per = ROW_GROUPS * ROW_UNROLL;
-    k_fp8_rows<T><<<(unsigned)((blocks + per - 1) / per), ROW_THREADS, 0, st>>>(x, a.row_stride, (int)a.cols, (int)kb, blocks, vec, a.pow2, a.codes, a.code_stride,
-                                                                               a.scale, a.scale_row_stride, a.scale_col_stride);
+    const long kb = (a.cols + FP8_BLOCK - 1) / FP8_BLOCK, tiles = (a.rows + ROW_TILE - 1) / ROW_TILE * kb;
+    k_fp8_rows<T><<<(unsigned)tiles, ROW_THREADS, 0, st>>>(x, a.row_stride, a.rows, (int)a.cols, (int)kb, vec, a.pow2, a.codes, a.code_stride, a.scale,
+                                                           a.scale_row_stride, a.scale_col_stride);
   } else {
     const long ct = (a.cols + TILE - 1) / TILE, tiles = ct * ((a.rows + TILE - 1) / TILE);
     auto run = [&](auto kernel) {
