@@ -238,20 +238,20 @@ inline bool rows_aligned(const void* p, long stride, size_t size) {
 // Stages of `stage_bytes` for the workers of a CTA, of which `ctas` at most share an SM: fewer CTAs where not even two stages fit, and
 // no ring (0) where a single CTA has no room for them.
 constexpr int RING_BYTES_PER_SM = 150 * 1024;
-inline int ring_stages(long stage_bytes, int workers, int& ctas) {
+inline int ring_stages(long stage_bytes, int workers, int& ctas, long bytes_per_sm = RING_BYTES_PER_SM) {
   for (; ctas > 0; --ctas) {
-    const long n = RING_BYTES_PER_SM / ctas / workers / stage_bytes;
+    const long n = bytes_per_sm / ctas / workers / stage_bytes;
     if (n >= 2) return n > MAX_STAGES ? MAX_STAGES : (int)n;
   }
   ctas = 1;
   return 0;
 }
 // per device, once: the kernel may have a ring's shared memory
-template <class K> inline void allow_ring(K* kernel, std::atomic<uint64_t>& done) {
+template <class K> inline void allow_ring(K* kernel, std::atomic<uint64_t>& done, int bytes = RING_BYTES_PER_SM) {
   int dev = 0;
   cudaGetDevice(&dev);
   if (done.load(std::memory_order_acquire) >> (dev & 63) & 1) return;
-  cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES_PER_SM);
+  cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   done.fetch_or(1ull << (dev & 63), std::memory_order_release);
 }
 

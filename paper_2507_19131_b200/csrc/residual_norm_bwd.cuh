@@ -312,6 +312,11 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), ctas_per_sm<TPR>()) k_resi
       for (int i = 0; i < VPT; ++i) store_floats<TPR, VEC>(out + (long)s * C, i, l, C, sums[s][i]);
 }
 
+// A ring for rows of which two do not fit into RING_BYTES_PER_SM, for CTAs that have their SM to themselves.  (Not for the others: what
+// the ring takes is lost to the L1, which has the parameters.  16384 x 4096 takes 364 us with it and 324 without, but 8000 x 8192 with a
+// binary32 stream, which has no ring otherwise, 412 instead of 705.)
+constexpr int WIDE_RING_BYTES = 200 * 1024;
+
 // ---- shapes ----------------------------------------------------------------------------------------------------------------
 struct Shape { int rows_per_cta; long ctas, per_worker; };
 template <int TPR> Shape shape_of(long rows) {
@@ -323,19 +328,22 @@ template <int TPR> Shape shape_of(long rows) {
   s.ctas = ((rows + s.per_worker - 1) / s.per_worker + s.rows_per_cta - 1) / s.rows_per_cta;
   return s;
 }
-// f(threads of a row, vectors of a thread, rows taken together), as constants.  Two rows at a time where their registers fit.
-template <class F> auto with_shape(int dim, F f) {
+// f(threads of a row, vectors of a thread, rows taken together), as constants.  Two rows at a time (WIDE_ROWS) where their registers fit and
+// two stages of them the ring: 16-bit rows in vector order (16384 x 4096 bfloat16: 324 us, one row at a time 339).  Others lose by it:
+// 16384 x 4096 with a binary32 stream 647 us by two, without a ring, and 405 by one; 10000 x 3001 bfloat16, element by element, 332 by two
+// and 239 by one.
+template <int WIDE_ROWS, class F> auto with_shape(int dim, F f) {
   using std::integral_constant;
   if (dim <= 256) return f(integral_constant<int, 32>{}, integral_constant<int, 1>{}, integral_constant<int, 1>{});
   if (dim <= 512) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{}, integral_constant<int, 1>{});
   if (dim <= 1024) return f(integral_constant<int, 128>{}, integral_constant<int, 1>{}, integral_constant<int, 1>{});
   if (dim <= 2048) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{}, integral_constant<int, 1>{});
-  if (dim <= 4096) return f(integral_constant<int, 512>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
+  if (dim <= 4096) return f(integral_constant<int, 512>{}, integral_constant<int, 1>{}, integral_constant<int, WIDE_ROWS>{});
   if (dim <= 8192) return f(integral_constant<int, 512>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
   return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
 }
 Shape shape_for(long rows, int dim) {
-  return with_shape(dim, [&](auto tpr, auto, auto) { return shape_of<decltype(tpr)::value>(rows); });
+  return with_shape<1>(dim, [&](auto tpr, auto, auto) { return shape_of<decltype(tpr)::value>(rows); });
 }
 }  // namespace
 
@@ -348,34 +356,40 @@ template <class TX, class TY> void residual_norm_bwd_typed(BwdParams q, cudaStre
              rows_aligned(a.gate, a.gate_stride, a.gate_f32 ? 4 : sizeof(TY)) && rows_aligned(g.dx_out, g.dx_out_stride, sizeof(TX)) &&
              rows_aligned(g.dh, g.dh_stride, sizeof(TY)) && rows_aligned(g.dx, g.dx_stride, sizeof(TX)) && rows_aligned(g.dy, g.dy_stride, sizeof(TY));
   for (const float* v : {a.post.gamma, a.post.beta, a.pre.gamma}) vec &= rows_aligned(v, 0, 4);
-  with_shape(a.dim, [&](auto tpr, auto vpt, auto rows) {
+  auto run_shape = [&](auto tpr, auto vpt, auto rows) {
     constexpr int TPR = decltype(tpr)::value, VPT = decltype(vpt)::value, ROWS = decltype(rows)::value;
     const uint32_t x = (uint32_t)(a.dim * sizeof(TX)), y = (uint32_t)(a.dim * sizeof(TY));
     q.x_bytes = vec ? staged_bytes<true>(x) : staged_bytes<false>(x);
     q.y_bytes = vec ? staged_bytes<true>(y) : staged_bytes<false>(y);
     q.stage_bytes = ROWS * 2 * (q.x_bytes + q.y_bytes);
-    int ctas = ctas_per_sm<TPR>();
+    int ctas = ctas_per_sm<TPR>(), ring_bytes = RING_BYTES_PER_SM;
     const int most = ctas;
-    q.stages = ring_stages(q.stage_bytes, cta_workers<TPR>(), ctas);
+    q.stages = ring_stages(q.stage_bytes, cta_workers<TPR>(), ctas, ring_bytes);
     if (ctas < most) q.stages = 0;                        // (the grid is sized for all)
+    if (TPR >= 512 && !q.stages) q.stages = ring_stages(q.stage_bytes, 1, ctas, ring_bytes = WIDE_RING_BYTES);
     auto run = [&](auto kernel, std::atomic<uint64_t>* done) {
-      if (done) allow_ring(kernel, *done);
+      if (done) allow_ring(kernel, *done, TPR >= 512 ? WIDE_RING_BYTES : RING_BYTES_PER_SM);
       launch_pdl(kernel, dim3((unsigned)s.ctas), cta_threads<TPR>(), (size_t)q.stages * q.stage_bytes * cta_workers<TPR>(), st, q);
       ++g_launches;
     };
-    // Rows of up to 2048 elements always have room for two stages; longer ones may not.
-    constexpr long widest = ROWS * 4L * ((TPR * VPT * 8 * 4 + 15) / 16 * 16 + 16);
-    static_assert(TPR >= 512 || RING_BYTES_PER_SM / ctas_per_sm<TPR>() / cta_workers<TPR>() / widest >= 2, "a ring for every short row");
-    if (TPR >= 512 && !q.stages) {
-      run(k_residual_norm_bwd<TX, TY, TPR, VPT, ROWS, false, (TPR < 512)>, nullptr);
-    } else if (vec) {
+    // Rows of up to 2048 elements always have room for two stages, and pairs of rows in 16 bits; longer ones may not.
+    constexpr long widest = ROWS * 2L * (TPR * VPT * 8) * (sizeof(TX) + sizeof(TY)) + ROWS * 4 * 32;
+    constexpr bool always = TPR < 512 || ROWS > 1;
+    static_assert(!always || RING_BYTES_PER_SM / ctas_per_sm<TPR>() / cta_workers<TPR>() / widest >= 2, "a ring for every short row");
+    if (ROWS == 1 && !always && !q.stages) {
+      run(k_residual_norm_bwd<TX, TY, TPR, VPT, 1, false, always>, nullptr);
+    } else if (ROWS > 1 || vec) {
       static std::atomic<uint64_t> done{0};
       run(k_residual_norm_bwd<TX, TY, TPR, VPT, ROWS, true, true>, &done);
     } else {
       static std::atomic<uint64_t> done{0};
-      run(k_residual_norm_bwd<TX, TY, TPR, VPT, ROWS, false, true>, &done);
+      run(k_residual_norm_bwd<TX, TY, TPR, VPT, 1, false, true>, &done);
     }
-  });
+  };
+  if constexpr (sizeof(TX) == 2) {
+    if (vec) { with_shape<2>(a.dim, run_shape); return; }
+  }
+  with_shape<1>(a.dim, run_shape);
 }
 
 }  // namespace mixaq

@@ -470,6 +470,13 @@ def test_norm_backward_types_and_widths(ctx, g, xt, yt, rows, dim):
     check_backward(ctx, Case(g, rows, dim, xt, yt, "rms", "layer"), g)
 
 
+@pytest.mark.parametrize("xt,yt", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("rows,dim", [(1037, 4096), (901, 3001), (1037, 2056), (1037, 8192), (901, 8191), (1037, 6000)])
+def test_norm_backward_refills_of_wide_rows(ctx, g, xt, yt, rows, dim):
+    """Six or seven rows a worker: every stage of a ring is filled again, and the last one has an odd row over."""
+    check_backward(ctx, Case(g, rows, dim, xt, yt, "layer", "layer", "sequence", 5, 0.5), g)
+
+
 @pytest.mark.parametrize("post", ["", "layer", "rms"])
 @pytest.mark.parametrize("pre", ["", "layer", "rms"])
 @pytest.mark.parametrize("gate,per,gate_f32", [("", None, False), ("channel", None, True), ("sequence", 7, False), ("sequence", 1000, True), ("token", None, False)])
