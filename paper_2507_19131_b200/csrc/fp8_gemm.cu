@@ -144,6 +144,27 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t addr, uint32_t rank) {
   return v;
 }
 
+// A block's sum is 0 or 2^-18 to 2^25 in magnitude (128 products of codes), so its product with a factor between 2^-100 and 2^100 is a normal
+// number.  Sums with a factor beyond, zeros apart, are scaled in binary64: two scales' product, or a sum's with one of them, may leave
+// binary32 where the result does not.  (NaN stays with the ordinary operations, which carry it on.)  Asking costs a k-block of a pair 26
+// cycles of 740: 8192^3 takes 489 us with it and 472 without.  (Asked a k-block ahead, beneath the sums or behind them, 499 to 505; behind the
+// wait for the sums 504.)
+__device__ __forceinline__ bool far_factor(float f, bool zero) {
+  const float m = fabsf(f);
+  return m > 0x1p100f || (m < 0x1p-100f && !zero);
+}
+// acc + d a w, rounded to binary32 once
+__device__ __forceinline__ float add_far(float acc, float d, float a, float w) {
+  return (float)__fma_rn((double)d, __dmul_rn((double)a, (double)w), (double)acc);
+}
+
+// c ? a : b, without a branch (which the compiler makes of it otherwise, and spills 300 bytes around 64 of them)
+__device__ __forceinline__ float choose(bool c, float a, float b) {
+  float r;
+  asm("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\tselp.f32 %0, %1, %2, p;\n\t}" : "=f"(r) : "f"(a), "f"(b), "r"((uint32_t)c));
+  return r;
+}
+
 // n (<= E) elements of a row to memory, as one piece where all are there and the address allows it
 template <class T, int E>
 __device__ __forceinline__ void store_piece(T* p, const T (&v)[E], bool vec, int n) {
@@ -416,37 +437,69 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         for (int i = 0; i + 1 < AHEAD_REGS; ++i) { a_next[i] = a_next[i + 1]; w_next[i] = w_next[i + 1]; }
         fetch(AHEAD_REGS - 1);
         if (COLSCALE && !mbar_wait_warp<true>(bar_cfull + 8u * (uint32_t)col_slot, col_pass, abort_flag)) { ok = false; break; }
+        const float* const cw = col_scales + col_slot * BN + half * COLS;
+        // the factor of the row's sums; columns with scales of their own have theirs in front of it
+        const float s0 = COLSCALE ? a0 : __fmul_rn(a0, w0);
+        bool far = false;
+        if constexpr (COLSCALE) {
+#pragma unroll
+          for (int i = 0; i < COLS; i += 32) {
+            const float w = cw[i + lane % (COLS < 32 ? COLS : 32)];
+            far |= far_factor(w, w == 0.0f);
+          }
+        } else {
+          far = far_factor(s0, a0 == 0.0f || w0 == 0.0f);
+        }
+        const bool any_far = __any_sync(0xffffffffu, far);
         if (!mbar_wait_warp<true>(bar_tfull + 8u * (uint32_t)slot, pass, abort_flag)) { ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem_q + (uint32_t)(slot * SLOT_COLS);
-        const float4* const cs = reinterpret_cast<const float4*>(col_scales + col_slot * BN + half * COLS);
-        float r[2][LD];
-        tmem_ld_rows(d, r[0]);
-        const float2 s = f2(COLSCALE ? a0 : __fmul_rn(a0, w0));
+        auto give_back = [&]() {                              // all is read: the tensor core may have the slot back
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (PAIR) arrive_cluster(tempty_at + 8u * (uint32_t)slot);
+            else mbar_arrive(bar_tempty + 8u * (uint32_t)slot);
+          }
+        };
+        if (!any_far) {
+          const float4* const cs = reinterpret_cast<const float4*>(cw);
+          float r[2][LD];
+          tmem_ld_rows(d, r[0]);
+          const float2 s = f2(s0);
 #pragma unroll
-        for (int c = 0; c < COLS; c += LD) {
-          float (&v)[LD] = r[(c / LD) & 1];
-          tmem_wait(v);
-          if (c + LD < COLS) {
-            tmem_ld_rows(d + (uint32_t)(c + LD), r[(c / LD + 1) & 1]);
-          } else {                                            // all is read: the tensor core may have the slot back
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) {
-              if constexpr (PAIR) arrive_cluster(tempty_at + 8u * (uint32_t)slot);
-              else mbar_arrive(bar_tempty + 8u * (uint32_t)slot);
+          for (int c = 0; c < COLS; c += LD) {
+            float (&v)[LD] = r[(c / LD) & 1];
+            tmem_wait(v);
+            if (c + LD < COLS) tmem_ld_rows(d + (uint32_t)(c + LD), r[(c / LD + 1) & 1]);
+            else give_back();
+#pragma unroll
+            for (int i = 0; i < LD; i += 4) {
+              float2 d0 = make_float2(v[i], v[i + 1]), d1 = make_float2(v[i + 2], v[i + 3]);
+              if (COLSCALE) {
+                const float4 w = cs[(c + i) / 4];
+                d0 = __fmul2_rn(d0, make_float2(w.x, w.y)); d1 = __fmul2_rn(d1, make_float2(w.z, w.w));
+              }
+              acc[(c + i) / 2] = __ffma2_rn(d0, s, acc[(c + i) / 2]);
+              acc[(c + i) / 2 + 1] = __ffma2_rn(d1, s, acc[(c + i) / 2 + 1]);
             }
           }
+        } else {
+          // rows and columns without such a factor get the same bits as above
 #pragma unroll
-          for (int i = 0; i < LD; i += 4) {
-            float2 d0 = make_float2(v[i], v[i + 1]), d1 = make_float2(v[i + 2], v[i + 3]);
-            if (COLSCALE) {
-              const float4 w = cs[(c + i) / 4];
-              d0 = __fmul2_rn(d0, make_float2(w.x, w.y)); d1 = __fmul2_rn(d1, make_float2(w.z, w.w));
+          for (int c = 0; c < COLS; c += 8) {
+            float v[8];
+            tmem_ld_rows(d + (uint32_t)c, v);
+            tmem_wait(v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float& t = i & 1 ? acc[(c + i) / 2].y : acc[(c + i) / 2].x;
+              const float w = COLSCALE ? cw[c + i] : w0;
+              const float near = __fmaf_rn(COLSCALE ? __fmul_rn(v[i], w) : v[i], s0, t);
+              t = choose(COLSCALE ? far_factor(w, w == 0.0f) : far, add_far(t, v[i], a0, w), near);
             }
-            acc[(c + i) / 2] = __ffma2_rn(d0, s, acc[(c + i) / 2]);
-            acc[(c + i) / 2 + 1] = __ffma2_rn(d1, s, acc[(c + i) / 2 + 1]);
           }
+          give_back();
         }
         if (COLSCALE) {
           __syncwarp();
