@@ -16,7 +16,6 @@
 #include "fp8.cuh"
 #include "tc_ptx.cuh"
 #include <atomic>
-#include <mutex>
 #include <cstring>
 
 namespace mixaq {
@@ -579,58 +578,56 @@ bool make_rows_map(CUtensorMap* m, const uint8_t* ptr, uint64_t rows, uint64_t c
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Per device, once: opt in to the shared memory, check that the register shares fit into what the block is launched with, and count
-// the clusters of 1, 2, 4 and 8 that run at once (a GPC's SMs are no multiple of a cluster, and chips differ in how many each GPC has).
-// Null on failure.
-struct AtOnce { int of[4]; };                    // by the logarithm of the cluster's size; 0 unless asked for
+// Per device, once: opt in to the shared memory, check that the register shares fit into what the block is launched with, and count the
+// CTAs or pairs that run at once.  0 on failure.
 template <int BN, bool COLSCALE>
-const AtOnce* set_up(int sms) {
+int set_up(int sms) {
   static_assert(smem_total(BN, COLSCALE) + 1024 <= 227 * 1024, "shared memory");
-  static AtOnce known[64];
-  static std::atomic<bool> ready[64];
-  static std::mutex lock;
+  static std::atomic<int> known[64];
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev > 63) return nullptr;
-  if (ready[dev].load(std::memory_order_acquire)) return &known[dev];
-  std::lock_guard<std::mutex> hold(lock);
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev > 63) return 0;
+  int at_once = known[dev].load(std::memory_order_acquire);
+  if (at_once) return at_once;
   cudaFuncAttributes at;
   const auto kernel = k_fp8_gemm<BN, COLSCALE>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_total(BN, COLSCALE) + 1024) != cudaSuccess ||
       cudaFuncGetAttributes(&at, kernel) != cudaSuccess)
-    return nullptr;
-  if (paired(BN) && FIRST_EPI * SIDE_REGS + EPI_WARPS * EPI_REGS > (FIRST_EPI + EPI_WARPS) * at.numRegs) return nullptr;
-  known[dev].of[0] = sms;
-  for (int log2 = 1; log2 <= (paired(BN) ? 1 : 3); ++log2) {
+    return 0;
+  if (paired(BN) && FIRST_EPI * SIDE_REGS + EPI_WARPS * EPI_REGS > (FIRST_EPI + EPI_WARPS) * at.numRegs) return 0;
+  at_once = sms;
+  if (paired(BN)) {
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 1u << log2; attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)(sms >> log2 << log2)); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = smem_total(BN, COLSCALE) + 1024;
+    attr.val.clusterDim.x = 2; attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(sms / 2 * 2)); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = smem_total(BN, COLSCALE) + 1024;
     cfg.attrs = &attr; cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) return nullptr;
-    known[dev].of[log2] = n;
+    if (cudaOccupancyMaxActiveClusters(&at_once, kernel, &cfg) != cudaSuccess || at_once < 1) return 0;
   }
-  ready[dev].store(true, std::memory_order_release);
-  return &known[dev];
+  known[dev].store(at_once, std::memory_order_release);
+  return at_once;
 }
 
-// Tile width and split.  A CTA (or pair) takes `block` microseconds a k-block and `store` a tile; a split adds its join.  The constants
+// Tile width and split, from the product's sizes alone: the split is the order in which k-blocks are added, and the same call gives the same
+// bits on every device.  A CTA (or pair) takes `block` microseconds a k-block and `store` a tile; a split adds its join.  The constants
 // were fitted to the times of all widths and splits at 17 shapes from 1 x 1024 x 8192 to 2048 x 4096 x 16384: the choice is the fastest measured
 // at 15 of them and within 6 % at the others.  (us: 1 x 4096 x 4096 by 128 columns in 4 parts 9.2, in 2 parts 10.1, whole 12.6, 32 columns
 // whole 16.4; 1024 x 4096 x 4096 by pairs 22, 128 columns 30; 300 x 1000 x 1000 by 32 columns 5.6, 128 columns 7.7.)  A split is
-// one round of clusters: where one too many waits for another to end the time doubles (16 clusters of 8 took 14.5 us where 8 took 7.2; 36
-// of 4 took 161 us on a chip that has room for 33 and 131 on one that has it; in two parts by 64 columns the same product takes 134).
+// one round of clusters: where one too many waits for another to end the time doubles (16 clusters of 8 took 14.5 us where 8 took 7.2).  A
+// GPC's SMs are no multiple of a cluster, and chips differ in how many each GPC has, so that AT_ONCE counts what the chip with the fewest had:
+// 1536 x 384 x 66800 takes 134 us in two parts by 64 columns everywhere, where a chip with room for 36 clusters of 4 takes 131 by 128 columns in
+// four, and one with room for 33 takes 161.
+constexpr int AT_ONCE[4] = {148, 74, 33, 15};     // clusters of 1, 2, 4 and 8 CTAs
 struct Plan { int bn, split; };
-Plan pick_plan(int M, int N, int k_blocks, const AtOnce& most) {
+Plan pick_plan(int M, int N, int k_blocks) {
   Plan best = {0, 0};
   double best_cost = 0.0;
   for (int bn = 32; bn <= 256; bn *= 2) {
-    const int rows = paired(bn) ? 2 * BM : BM, at_once = most.of[paired(bn) ? 1 : 0];
+    const int rows = paired(bn) ? 2 * BM : BM, at_once = AT_ONCE[paired(bn) ? 1 : 0];
     const long tiles = (long)((M + rows - 1) / rows) * ((N + bn - 1) / bn);
     const double block = bn == 256 ? 0.52 : bn == 128 ? 0.32 : bn == 64 ? 0.29 : 0.26, store = bn == 256 ? 3.0 : bn == 128 ? 1.7 : bn == 64 ? 1.0 : 0.7;
     for (int split = 1, log2 = 0; split <= MAX_SPLIT; split *= 2, ++log2) {
-      if (split > 1 && (paired(bn) || split > k_blocks || tiles > most.of[log2])) break;
+      if (split > 1 && (paired(bn) || split > k_blocks || tiles > AT_ONCE[log2])) break;
       const long rounds = split > 1 ? 1 : (tiles + at_once - 1) / at_once;
       const double cost = rounds * ((k_blocks + split - 1) / split * block + store) + (split > 1 ? 1.5 + 0.07 * split : 0.0);
       if (!best.bn || cost <= best_cost) { best = {bn, split}; best_cost = cost; }
@@ -641,9 +638,8 @@ Plan pick_plan(int M, int N, int k_blocks, const AtOnce& most) {
 
 template <int BN, bool COLSCALE>
 bool launch_as(const Params& p, cudaStream_t st, int sms) {
-  const AtOnce* most = set_up<BN, COLSCALE>(sms);
-  if (!most) return false;
-  const int at_once = most->of[paired(BN) ? 1 : 0];
+  const int at_once = set_up<BN, COLSCALE>(sms);
+  if (!at_once) return false;
   CUtensorMap mA, mW;
   if (!make_rows_map(&mA, p.g.a.codes, p.M, p.g.K, p.g.a.stride, BM) ||
       !make_rows_map(&mW, p.g.w.codes, p.N, p.g.K, p.g.w.stride, paired(BN) ? 64 : BN))
@@ -670,9 +666,7 @@ bool launch_fp8_matmul(const Fp8MatmulArgs& g, cudaStream_t st) {
   p.g = g; p.M = (int)g.a.rows; p.N = (int)g.w.rows;
   p.k_blocks = (int)((g.K + BK - 1) / BK);
   const int sms = sm_count();
-  const AtOnce* most = set_up<64, false>(sms);   // (every instance has an SM to itself, so the counts are the same for all)
-  if (!most) return false;
-  const Plan plan = pick_plan(p.M, p.N, p.k_blocks, *most);
+  const Plan plan = pick_plan(p.M, p.N, p.k_blocks);
   p.m_tiles = (p.M + (paired(plan.bn) ? 2 * BM : BM) - 1) / (paired(plan.bn) ? 2 * BM : BM);
   p.n_tiles = (p.N + plan.bn - 1) / plan.bn;
   if ((long)p.m_tiles * p.n_tiles >= (1L << 31) - sms) return false;
