@@ -1,15 +1,15 @@
-"""The row operators on the GPU where the first set of tests does not go: scales of the product at both ends of binary32's range.
-Tolerances are counted as in test_gpu_row_ops.py, whose definitions these tests share."""
+"""The row operators on the GPU where the first set of tests does not go: scales of the product at both ends of binary32's range, and
+gradients written over what they are made from.  Tolerances are counted as in test_gpu_row_ops.py, whose definitions these tests share."""
 import pytest
 import torch
 
 from paper_2507_19131_b200 import binding as mq
-from test_gpu_row_ops import E4M3, TYPES, U, codes_of, ctx, g, matmul_reference, normal, rounding, within  # noqa: F401 (fixtures)
+from test_gpu_row_ops import E4M3, TYPES, U, Case, codes_of, ctx, g, matmul_reference, normal, rounding, within  # noqa: F401 (fixtures)
 
 pytestmark = pytest.mark.gpu
 
-# parts of a cluster, single CTAs, pairs of CTAs; a k-block that is not full
-SHAPES = [(40, 300, 1100), (300, 520, 1000), (1000, 64, 5000), (5000, 4300, 700)]
+# every width of tile, parts of a cluster, single CTAs, pairs of CTAs; a k-block that is not full
+SHAPES = [(40, 300, 1100), (300, 520, 1000), (1000, 64, 5000), (9, 4096, 2100), (5000, 4300, 700)]
 
 
 def check_far(ctx, a, w, dtype="f32"):
@@ -76,3 +76,49 @@ def test_far_scales_change_their_own_outputs_only(ctx, g, m, n, k, w_rows):
     rows = torch.arange(m, device="cuda") != 5
     assert torch.equal(y[rows][:, w_rows:], z[rows][:, w_rows:])
     check_far(ctx, a, w)
+
+
+# ---- gradients over what they are made from ------------------------------------------------------------------------------------
+def backward_into(ctx, c, x, y, dx_out, dh, dx, dy):
+    """mixaq_residual_norm_backward through the C interface, dx and dy at given places; returns the parameters' gradients."""
+    rows, dim = c.rows, c.dim
+    def place(t):
+        return t.data_ptr(), t.stride(0)
+    gate = mq._gate_fields(ctx, c.gate, c.per, rows, dim, c.yt)
+    dgate = torch.full((gate[4], dim), torch.nan, device="cuda")
+    sums = torch.full((4, dim), torch.nan, device="cuda")
+    p = mq._NORM_PARAMS.pack(rows, dim, mq._DTYPES[c.xt], mq._DTYPES[c.yt], gate[1], *place(x), *place(y), gate[0], gate[2], gate[3], c.scale,
+                             *mq._norm_fields(ctx, c.post, dim, "post"), *mq._norm_fields(ctx, c.pre, dim, "pre"), 0, 0, 0, 0, 0)
+    at = mq._NORM_GRADS.pack(*place(dx_out), *place(dh), *place(dx), *place(dy), dgate.data_ptr(), dim, *(s.data_ptr() for s in sums))
+    work = torch.empty(mq.lib().mixaq_residual_norm_backward_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    ctx.check(mq.lib().mixaq_residual_norm_backward(ctx.h, p, at, work.data_ptr(), work.numel(), mq._stream()), "residual_norm_backward")
+    return dgate, sums
+
+
+@pytest.mark.parametrize("xt,yt", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("rows,dim,pad,odd", [(1, 96, 0, 0), (3000, 96, 0, 0), (1037, 257, 3, 1), (1037, 1001, 0, 1), (1037, 2048, 8, 8), (1037, 4096, 0, 0), (901, 3001, 1, 3),
+                                              (301, 8192, 0, 0), (301, 8191, 5, 1), (200, 16384, 0, 0), (160, 16383, 0, 0)])
+def test_gradients_in_place(ctx, g, xt, yt, rows, dim, pad, odd):
+    """dx over dx_out, dy over dh or over y: the same bits as apart, and nothing beside the rows written."""
+    c = Case(g, rows, dim, xt, yt, "rms", "layer", "sequence", 5, 0.5, pad=pad, odd=odd)
+    dx_out, dh = c.rows_of(c.xt), c.rows_of(c.yt)
+    dx_out.copy_(normal(g, rows, dim))
+    dh.copy_(normal(g, rows, dim) * 0.5)
+
+    def copy(t):
+        u = c.rows_of(t.dtype)
+        u.copy_(t)
+        return u
+    dx, dy = c.rows_of(c.xt), c.rows_of(c.yt)
+    want = backward_into(ctx, c, c.x, c.y, dx_out, dh, dx, dy)
+    assert not any(bool(torch.isnan(t).any()) for t in (dx, dy, want[0], want[1][[0, 2, 3]]))
+    for over in ("dh", "y"):
+        x1, y1, dxo1, dh1 = copy(c.x), copy(c.y), copy(dx_out), copy(dh)
+        dy1 = dh1 if over == "dh" else y1
+        got = backward_into(ctx, c, x1, y1, dxo1, dh1, dxo1, dy1)
+        assert torch.equal(dxo1, dx) and torch.equal(dy1, dy) and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert torch.equal(x1, c.x) and torch.equal(dh1 if over == "y" else y1, dh if over == "y" else c.y)
+        for t in (dxo1, dy1):
+            beside = torch.ones(t.untyped_storage().nbytes() // t.element_size(), dtype=torch.bool, device="cuda")
+            torch.as_strided(beside, t.shape, t.stride(), t.storage_offset()).fill_(False)
+            assert bool(torch.isnan(torch.as_strided(t, beside.shape, (1,), 0)[beside]).all())
