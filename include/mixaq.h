@@ -225,7 +225,9 @@ mixaq_status mixaq_norm_forward(mixaq_ctx* ctx, const float* gamma, const float*
 /* ---- row operators: 8-bit floating-point codes with block scales, their product, and the norms at a sublayer's border.
  *      They work on row-major matrices of any size; a row stride is a number of elements, strides and row counts are 64-bit.
  *      The context's device has to be the current one.  A call with no rows returns MIXAQ_OK without a launch.  Calls use no memory
- *      beyond their arguments, may be captured, and what lies behind a matrix's last row or last column is neither read nor written. ---- */
+ *      beyond their arguments and may be captured.  What lies behind a matrix's last row, or behind the last column of its rows, is not
+ *      written and enters no result.  It is not read either, but for one case: the norms copy rows that do not start and end on 16-byte
+ *      boundaries with up to 15 bytes on each side, between the matrix's first element and its last. ---- */
 typedef enum { MIXAQ_F32 = 0, MIXAQ_BF16 = 1, MIXAQ_F16 = 2 } mixaq_dtype;
 
 /* A matrix of e4m3 codes (4 exponent bits, bias 7, 3 mantissa bits, no infinities, largest value 448) with one binary32 scale for each

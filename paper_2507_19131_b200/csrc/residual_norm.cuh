@@ -90,7 +90,7 @@ __device__ __forceinline__ float sum8(const F8& f, float2 t) {
 
 // One matrix whose rows pass through the ring
 struct RowSource { const uint8_t* base; const uint8_t* end; long stride; uint32_t bytes; };      // bytes: of a row, stride and end too
-template <class T> __device__ __forceinline__ RowSource row_source(const void* p, long stride, long rows, int dim) {
+template <class T> __host__ __device__ __forceinline__ RowSource row_source(const void* p, long stride, long rows, int dim) {
   const uint8_t* b = static_cast<const uint8_t*>(p);
   const uint32_t bytes = (uint32_t)(dim * sizeof(T));
   return {b, b + ((rows - 1) * stride * (long)sizeof(T) + bytes), stride * (long)sizeof(T), bytes};
@@ -99,7 +99,7 @@ template <class T> __device__ __forceinline__ RowSource row_source(const void* p
 template <bool VEC> __host__ __device__ __forceinline__ uint32_t staged_bytes(uint32_t row_bytes) { return VEC ? row_bytes : (row_bytes + 15) / 16 * 16 + 16; }
 // what is copied of a row
 struct RowSpan { const uint8_t *start, *lo, *hi; };
-template <bool VEC> __device__ __forceinline__ RowSpan row_span(const RowSource& s, long row) {
+template <bool VEC> __host__ __device__ __forceinline__ RowSpan row_span(const RowSource& s, long row) {
   RowSpan r;
   r.start = s.base + row * s.stride;
   if (VEC) { r.lo = r.start; r.hi = r.start + s.bytes; return r; }
