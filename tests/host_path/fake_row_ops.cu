@@ -6,6 +6,7 @@ extern "C" {
 mixaq::Fp8QuantArgs last_quantize;
 mixaq::Fp8MatmulArgs last_matmul;
 mixaq::ResNormArgs last_norm;
+mixaq::ResNormGradArgs last_grads;
 int fail_matmul;                                          // the launch's set-up fails while this is set
 }
 
@@ -18,5 +19,5 @@ bool launch_fp8_matmul(const Fp8MatmulArgs& g, cudaStream_t st) {
 }
 void launch_residual_norm(const ResNormArgs& a, int*, cudaStream_t st) { last_norm = a; ++g_launches; enqueue(st); }
 size_t residual_norm_backward_floats(long rows, int dim, bool per_sequence) { return (size_t)(rows > 0 ? 5 * dim : 64) * (per_sequence ? 2 : 1); }
-void launch_residual_norm_backward(const ResNormArgs& a, const ResNormGradArgs&, int*, cudaStream_t st) { last_norm = a; ++g_launches; enqueue(st); }
+void launch_residual_norm_backward(const ResNormArgs& a, const ResNormGradArgs& g, int*, cudaStream_t st) { last_norm = a; last_grads = g; ++g_launches; enqueue(st); }
 }  // namespace mixaq

@@ -122,3 +122,16 @@ def test_gradients_in_place(ctx, g, xt, yt, rows, dim, pad, odd):
             beside = torch.ones(t.untyped_storage().nbytes() // t.element_size(), dtype=torch.bool, device="cuda")
             torch.as_strided(beside, t.shape, t.stride(), t.storage_offset()).fill_(False)
             assert bool(torch.isnan(torch.as_strided(t, beside.shape, (1,), 0)[beside]).all())
+
+
+@pytest.mark.parametrize("per", [601, (1 << 32) - 1, 1 << 32, 1 << 40])
+def test_a_sequence_longer_than_the_batch(ctx, g, per):
+    c = Case(g, 600, 264, "f32", "bf16", "rms", "layer", "channel")
+    dx_out, dh = normal(g, 600, 264), normal(g, 600, 264).bfloat16()
+    want = mq.residual_norm_forward(ctx, c.x, c.y, **c.args)
+    grads = mq.residual_norm_backward(ctx, want.x, c.y, dx_out=dx_out, dh=dh, **c.args)
+    c.args["rows_per_gate"] = per
+    got = mq.residual_norm_forward(ctx, c.x, c.y, **c.args)
+    assert torch.equal(got.x, want.x) and torch.equal(got.h, want.h)
+    for name, value in vars(mq.residual_norm_backward(ctx, want.x, c.y, dx_out=dx_out, dh=dh, **c.args)).items():
+        assert value is None or torch.equal(value, getattr(grads, name)), name
