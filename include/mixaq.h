@@ -234,8 +234,8 @@ typedef enum { MIXAQ_F32 = 0, MIXAQ_BF16 = 1, MIXAQ_F16 = 2 } mixaq_dtype;
  * block of `block_rows` rows (1 or 128) by 128 columns, counted from the matrix's corner; blocks at the edges are smaller.
  *   value(r, c) = codes[r*row_stride + c] * scale[(r/block_rows)*scale_row_stride + (c/128)*scale_col_stride]
  * codes are 16-byte aligned and row_stride is a multiple of 16 and at least cols (the TMA unit reads them); scales are 4-byte aligned
- * and lie in any order (for single rows scale_row_stride = 1 is fastest); as an output, no two may share a place.  rows and cols are
- * below 2^31 - 256, row_stride below 2^40. */
+ * and lie in any order (for single rows scale_row_stride = 1 is fastest with many output tiles, scale_col_stride = 1 with few of them and
+ * many columns); as an output, no two may share a place.  rows and cols are below 2^31 - 256, row_stride below 2^40. */
 typedef struct {
   uint8_t* codes; int64_t rows, cols, row_stride;
   int block_rows;
@@ -263,11 +263,13 @@ mixaq_status mixaq_fp8_matmul(mixaq_ctx* ctx, const mixaq_fp8_matrix* a, const m
  *   h     = norm_pre(x_out)                          (of the rounded x_out: the same as two calls)
  * x, x_out: the residual stream; y: what a sublayer returned; h: the input of the next one, in y_dtype or as e4m3 codes.
  *   norm MIXAQ_NORM_NONE: v;  MIXAQ_NORM_LAYER: gamma (v - mean) / sqrt(var + eps) + beta;  MIXAQ_NORM_RMS: gamma v / sqrt(mean(v^2) + eps) + beta
- * gamma and beta are binary32 [dim]; NULL stands for ones and zeros.  eps > 0.
+ * gamma and beta are binary32 [dim]; NULL stands for ones and zeros.  eps > 0.  Sums over a row are binary32: a row whose (deviations')
+ * squares add up to more than 3.4e38 is divided by infinity.
  * The gate of row r is row r / rows_per_gate of `gate`: rows_per_gate >= rows is a gate per channel, the length of a sequence a gate
  * per sequence, 1 a gate per token; gate == NULL: ones.
  * y == NULL: x_out = x, only h is computed; gate, post and x_out are NULL, NONE and NULL then.  h_fp8 != NULL: h is quantized as by
- * mixaq_fp8_quantize into this matrix (block_rows 1) in place of p->h, which is NULL then.  pre.kind NONE: no h (both NULL).
+ * mixaq_fp8_quantize, from binary32, into this matrix (block_rows 1) in place of p->h, which is NULL then.  pre.kind NONE: no h (both
+ * NULL).
  * x_out may be x, and h may be y (same address and stride); no other outputs may overlap.  1 <= dim <= MIXAQ_NORM_MAX_DIM.
  * Pointers need the alignment of their elements; 16-byte aligned rows and a dim that is a multiple of 8 run fastest.
  * Type pairs (x, y): (F32, any), (BF16, BF16), (F16, F16).  gate_dtype: y_dtype or MIXAQ_F32. */

@@ -564,7 +564,7 @@ def backbone_forward(ctx: Context, dbb: DeviceBackbone, x0: torch.Tensor, low_ra
 # ---- row operators: e4m3 codes with block scales, their product, the norms at a sublayer's border ---------------------------------
 # Structs are packed, not built field by field: these calls are short (a matmul's host work is 12 us, 4 of them the launch).
 FP8_BLOCK = 128
-NORM_MAX_DIM = 16384
+NORM_MAX_DIM = 16384                                                              # MIXAQ_NORM_MAX_DIM
 _E4M3, _F32 = torch.float8_e4m3fn, torch.float32
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _NORM_KINDS = {"layer": 1, "rms": 2}

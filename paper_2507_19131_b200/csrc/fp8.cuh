@@ -20,25 +20,11 @@ template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return
 
 // Eight consecutive elements as they lie in memory
 template <class T> struct Vec8 { T v[8]; };
-template <class T> __device__ __forceinline__ void load_vec8(const T* p, Vec8<T>& r) {      // p 16-byte aligned
-  uint4* d = reinterpret_cast<uint4*>(&r);
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(Vec8<T>) / 16; ++i) d[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
-}
-// the same element by element, zeros from element `n` on (n may be 0 or less)
-template <class T> __device__ __forceinline__ void load_some8(const T* p, int n, Vec8<T>& r) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) r.v[i] = i < n ? __ldg(p + i) : from_f32<T>(0.0f);
-}
 // a load of memory that the kernel itself may write later (rows updated in place); p 16-byte aligned
 template <class T> __device__ __forceinline__ void load_row8(const T* p, Vec8<T>& r) {
   uint4* d = reinterpret_cast<uint4*>(&r);
 #pragma unroll
   for (int i = 0; i < (int)sizeof(Vec8<T>) / 16; ++i) d[i] = reinterpret_cast<const uint4*>(p)[i];
-}
-template <class T> __device__ __forceinline__ void unpack8(const Vec8<T>& r, float (&f)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = to_f32(r.v[i]);
 }
 // max(|a|, |b|), no number if either is none (the sign of the result means nothing)
 __device__ __forceinline__ float max_abs(float a, float b) {

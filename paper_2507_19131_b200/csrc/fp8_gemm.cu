@@ -5,7 +5,8 @@
 // The scales change from k-block to k-block, so the tensor memory holds one k-block's sums d_b at a time and the epilogue warps keep the
 // running sums in registers: per k-block they read d_b (tcgen05.ld) and add scale * d_b with packed fused multiply-adds, while the tensor
 // core fills the next accumulator.  A k-block of a 128 x BN tile takes the tensor core BN cycles (8 192 multiply-adds a cycle and SM) and
-// the FMA pipe BN / 2 (128 packed lanes a cycle): the sums fit beneath the MMAs.
+// the FMA pipe BN / 2 (128 packed lanes a cycle).  What bounds it is neither, but the way of an accumulator: full, read, summed, free, next
+// MMA.  A pair's k-block takes 740 cycles where its MMAs are 512 (2048 x 4096 x 16384: 134 us, 2.05 PFLOP/s; 8192^3: 489 us, 2.25).
 //
 // One CTA per SM walks over 128 x BN output tiles: warp 0 feeds a ring of 128-byte-swizzled stages by TMA (no multicast), warp 1 issues
 // the MMAs, warp 2 brings a k-block's column scales to shared memory where weights have a scale per row, warps 4-11 are the epilogue
@@ -40,8 +41,10 @@ __host__ __device__ constexpr int stage_bytes(int bn) { return A_BYTES + w_rows(
 __host__ __device__ constexpr int ring_stages(int bn) { return bn >= 128 ? 6 : MAX_RING; }
 // Pairs keep 128 sums a thread: the side warpgroup gives up registers for them (4 x 72 + 8 x 216 of 12 x 168).
 constexpr int SIDE_REGS = 72, EPI_REGS = 216;
-// Scales come from memory long before their k-block: a latency of 800 cycles out of the L2 and 1 500 out of memory stands against 256 to
-// 512 cycles of a k-block (read two k-blocks ahead, every tile width took 750 cycles a k-block).  AHEAD k-blocks are under way.
+// Scales come long before their k-block: a latency of 800 cycles out of the L2 and 1 500 out of memory stands against 256 to 512 cycles of a
+// k-block (read two k-blocks ahead, every tile width took 750 cycles a k-block).  AHEAD k-blocks of the columns' scales are under way to
+// shared memory; of the rows' scales, and of weights' with 128 rows, AHEAD_REGS (4, below) are under way to registers.  Four do not cover
+// the latency where tiles are few and k-blocks many: 1536 x 384 x 66800 takes 121 us, and 90 with one scale for all of a's rows.
 constexpr int AHEAD = 8;
 // stage full, empty; slot full, empty; column scales full, empty; drain
 constexpr int NUM_BARS = 2 * MAX_RING + 2 * MAX_SLOTS + 2 * AHEAD + 1;

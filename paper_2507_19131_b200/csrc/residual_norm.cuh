@@ -145,9 +145,9 @@ __device__ __forceinline__ F8 load_gate(const ResNormArgs& p, long gate_row, int
 }
 
 // Sums over a row, N (1, 2 or 4) values at a time.  In a warp the first steps exchange halves of the values instead of adding all of
-// them everywhere, so that N values take little more than one: 5 + N - 1 shuffles, lane P k (P = 32 / N) ends with value k.  More than a
-// warp: one exchange through shared memory, and again.  The buffers alternate: a warp that is at the reduction after the next has
-// passed the barrier of the next one, which every warp reaches after it has read this one's sums.
+// them everywhere: N - 1 shuffles for that, log2 P more (P = 32 / N) until lane P k has value k, N to hand them out; 5, 7 and 10 for one,
+// two and four values.  More than a warp: one exchange through shared memory, and again.  The buffers alternate: a warp that is at the
+// reduction after the next has passed the barrier of the next one, which every warp reaches after it has read this one's sums.
 template <int TPR, int N>
 struct RowReduce {
   float (*slots)[N][TPR / 32];                 // [2][N][warps of the row]
