@@ -6,12 +6,13 @@
 // running sums in registers: per k-block they read d_b (tcgen05.ld) and add scale * d_b with packed fused multiply-adds, while the tensor
 // core fills the next accumulator.  A k-block of a 128 x BN tile takes the tensor core BN cycles (8 192 multiply-adds a cycle and SM) and
 // the FMA pipe BN / 2 (128 packed lanes a cycle).  What bounds it is neither, but the way of an accumulator: full, read, summed, free, next
-// MMA.  A pair's k-block takes 740 cycles where its MMAs are 512 (2048 x 4096 x 16384: 134 us, 2.05 PFLOP/s; 8192^3: 489 us, 2.25).
+// MMA.  A pair's k-block takes 730 cycles where its MMAs are 512 (2048 x 4096 x 16384: 131 us, 2.1 PFLOP/s; 8192^3: 474 us, 2.3).
 //
 // One CTA per SM walks over 128 x BN output tiles: warp 0 feeds a ring of 128-byte-swizzled stages by TMA (no multicast), warp 1 issues
-// the MMAs, warp 2 brings a k-block's column scales to shared memory where weights have a scale per row, warps 4-11 are the epilogue
-// (warp w has rows 32 (w % 4) ... of the tile and half of its columns).  Where there are few tiles, a cluster of up to 8 CTAs divides
-// the k-blocks of a tile and adds its parts through distributed shared memory, in the order of the ranks.
+// the MMAs, warp 2 brings a k-block's column scales to shared memory where weights have a scale per row, warp 3 looks for ones far from
+// one among them, warps 4-11 are the epilogue (warp w has rows 32 (w % 4) ... of the tile and half of its columns).  Where there are few
+// tiles, a cluster of up to 8 CTAs divides the k-blocks of a tile and adds its parts through distributed shared memory, in the order of
+// the ranks.
 // Every wait on an mbarrier is bounded, as in gemm_tc.cu.
 #include "kernels.h"
 #include "fp8.cuh"
@@ -46,11 +47,11 @@ constexpr int SIDE_REGS = 72, EPI_REGS = 216;
 // shared memory; of the rows' scales, and of weights' with 128 rows, AHEAD_REGS (4, below) are under way to registers.  Four do not cover
 // the latency where tiles are few and k-blocks many: 1536 x 384 x 66800 takes 121 us, and 90 with one scale for all of a's rows.
 constexpr int AHEAD = 8;
-// stage full, empty; slot full, empty; column scales full, empty; drain
-constexpr int NUM_BARS = 2 * MAX_RING + 2 * MAX_SLOTS + 2 * AHEAD + 1;
+// stage full, empty; slot full, empty; column scales full, looked at, empty; drain
+constexpr int NUM_BARS = 2 * MAX_RING + 2 * MAX_SLOTS + 3 * AHEAD + 1;
 
 __host__ __device__ constexpr int smem_total(int bn, bool cols) {
-  return ring_stages(bn) * stage_bytes(bn) + EPI_WARPS * STAGING + (cols ? AHEAD * bn * 4 : 0) + NUM_BARS * 8 + 16;
+  return ring_stages(bn) * stage_bytes(bn) + EPI_WARPS * STAGING + (cols ? AHEAD * (bn * 4 + 4) : 0) + NUM_BARS * 8 + 16;
 }
 
 struct Params {
@@ -132,6 +133,13 @@ __device__ __forceinline__ void tmem_wait(float (&r)[N]) {
     asm volatile("" : "+f"(r[i]), "+f"(r[i + 1]), "+f"(r[i + 2]), "+f"(r[i + 3]), "+f"(r[i + 4]), "+f"(r[i + 5]), "+f"(r[i + 6]), "+f"(r[i + 7]));
 }
 
+// eight columns of the warp's 32 rows, and the wait for all stores
+__device__ __forceinline__ void tmem_st_rows(uint32_t taddr, const float (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+      ::"f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
 __device__ __forceinline__ void cp_async4(uint32_t dst, const float* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -147,20 +155,31 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t addr, uint32_t rank) {
 }
 
 // A block's sum is 0 or 2^-18 to 2^25 in magnitude (128 products of codes), so its product with a factor between 2^-100 and 2^100 is a normal
-// number.  Sums with a factor beyond, zeros apart, are scaled in binary64: two scales' product, or a sum's with one of them, may leave
-// binary32 where the result does not.  (NaN stays with the ordinary operations, which carry it on.)  Asking costs a k-block of a pair 26
-// cycles of 740: 8192^3 takes 489 us with it and 472 without.  (Asked a k-block ahead, beneath the sums or behind them, 499 to 505; behind the
-// wait for the sums 504.)
+// number.  With a factor beyond, zeros apart, two scales' product, or a sum's with one of them, may leave binary32 where the result does
+// not: k-blocks that have such a factor take a way of their own, on which rows and columns without one get the same bits as otherwise.  (NaN
+// stays with the ordinary operations, which carry it on.)  The branch costs more than the question: 8192^3 takes 474 us with it and 466
+// without, 2048 x 4096 x 4096 with a scale per row of the weights 55.1 and 50.6.  (8192^3 with the branch in front of the first load of tensor
+// memory 482; with the question put a k-block ahead 499 to 505.  The latter, asked by the epilogue instead of a warp of its own, 58.9.)
 __device__ __forceinline__ bool far_factor(float f, bool zero) {
   const float m = fabsf(f);
   return m > 0x1p100f || (m < 0x1p-100f && !zero);
+}
+// a w as two factors of about the same exponent: neither is infinite, and a sum times the first is normal if the result is.  (Exponents
+// beyond +-250 end in infinity or zero all the same.)
+__device__ __forceinline__ void split_factor(float a, float w, float& first, float& second) {
+  const double p = __dmul_rn((double)a, (double)w);
+  const int e = (int)((uint64_t)__double_as_longlong(p) >> 52 & 2047) - 1023;
+  if (e > 1023) { first = (float)p; second = 1.0f; return; }                // an infinite scale
+  const int c = max(min(e, 250), -250), h = c / 2;
+  first = (float)__dmul_rn(p, __longlong_as_double((long long)(1023 + h - e) << 52));
+  second = __int_as_float((127 + c - h) << 23);
 }
 // acc + d a w, rounded to binary32 once
 __device__ __forceinline__ float add_far(float acc, float d, float a, float w) {
   return (float)__fma_rn((double)d, __dmul_rn((double)a, (double)w), (double)acc);
 }
 
-// c ? a : b, without a branch (which the compiler makes of it otherwise, and spills 300 bytes around 64 of them)
+// c ? a : b, without a branch (which the compiler makes of it otherwise, and spills 300 bytes around 128 of them)
 __device__ __forceinline__ float choose(bool c, float a, float b) {
   float r;
   asm("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\tselp.f32 %0, %1, %2, p;\n\t}" : "=f"(r) : "f"(a), "f"(b), "r"((uint32_t)c));
@@ -271,9 +290,10 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
   uint64_t* const bars = reinterpret_cast<uint64_t*>(col_scales + (COLSCALE ? AHEAD * BN : 0));
   const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8u * MAX_RING, bar_tfull = bar_empty + 8u * MAX_RING;
   const uint32_t bar_tempty = bar_tfull + 8u * MAX_SLOTS, bar_cfull = bar_tempty + 8u * MAX_SLOTS, bar_cempty = bar_cfull + 8u * AHEAD;
-  const uint32_t bar_drain = bar_cempty + 8u * AHEAD;
+  const uint32_t bar_clooked = bar_cempty + 8u * AHEAD, bar_drain = bar_clooked + 8u * AHEAD;
   uint32_t* const tmem_holder = reinterpret_cast<uint32_t*>(bars + NUM_BARS);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  int* const cols_far = reinterpret_cast<int*>(tmem_holder + 2);        // [AHEAD]: whether a k-block's column scales have a far one
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   uint32_t fills = 0;                          // TMA warp: fills of ring stages so far
 
@@ -286,7 +306,7 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
     for (int a = 0; a < MAX_SLOTS; ++a) {
       mbar_init(bar_tfull + 8u * a, 1u); mbar_init(bar_tempty + 8u * a, SLOT_WARPS * (PAIR ? 2u : 1u));
     }
-    for (int a = 0; a < AHEAD; ++a) { mbar_init(bar_cfull + 8u * a, 32u); mbar_init(bar_cempty + 8u * a, EPI_WARPS); }
+    for (int a = 0; a < AHEAD; ++a) { mbar_init(bar_cfull + 8u * a, 32u); mbar_init(bar_clooked + 8u * a, 1u); mbar_init(bar_cempty + 8u * a, EPI_WARPS); }
     mbar_init(bar_drain, 1u);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -387,6 +407,23 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (COLSCALE && warp == 3) {
+    // ---- are there far ones among them? ----
+    Ring cp;
+    bool ok = true;
+    for (int t = first; t < p.tiles && ok; t += step)
+      for (int kb = kb0; kb < kb1; ++kb, cp.next(AHEAD)) {
+        if (!mbar_wait_warp(bar_cfull + 8u * (uint32_t)cp.slot, cp.pass, abort_flag)) { ok = false; break; }
+        bool far = false;
+#pragma unroll
+        for (int i = 0; i < BN / 32; ++i) {
+          const float w = col_scales[cp.slot * BN + i * 32 + lane];
+          far |= far_factor(w, w == 0.0f);
+        }
+        far = __any_sync(0xffffffffu, far);
+        if (lane == 0) { cols_far[cp.slot] = far; mbar_arrive(bar_clooked + 8u * (uint32_t)cp.slot); }
+        __syncwarp();
+      }
   } else if (warp >= FIRST_EPI) {
     // ---- sums in registers, output ----
     if (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(EPI_REGS));
@@ -438,21 +475,12 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
 #pragma unroll
         for (int i = 0; i + 1 < AHEAD_REGS; ++i) { a_next[i] = a_next[i + 1]; w_next[i] = w_next[i + 1]; }
         fetch(AHEAD_REGS - 1);
-        if (COLSCALE && !mbar_wait_warp<true>(bar_cfull + 8u * (uint32_t)col_slot, col_pass, abort_flag)) { ok = false; break; }
+        if (COLSCALE && !mbar_wait_warp<true>(bar_clooked + 8u * (uint32_t)col_slot, col_pass, abort_flag)) { ok = false; break; }
         const float* const cw = col_scales + col_slot * BN + half * COLS;
         // the factor of the row's sums; columns with scales of their own have theirs in front of it
-        const float s0 = COLSCALE ? a0 : __fmul_rn(a0, w0);
-        bool far = false;
-        if constexpr (COLSCALE) {
-#pragma unroll
-          for (int i = 0; i < COLS; i += 32) {
-            const float w = cw[i + lane % (COLS < 32 ? COLS : 32)];
-            far |= far_factor(w, w == 0.0f);
-          }
-        } else {
-          far = far_factor(s0, a0 == 0.0f || w0 == 0.0f);
-        }
-        const bool any_far = __any_sync(0xffffffffu, far);
+        float s0 = COLSCALE ? a0 : __fmul_rn(a0, w0);
+        const bool far = COLSCALE ? cols_far[col_slot] : far_factor(s0, a0 == 0.0f || w0 == 0.0f);
+        const bool any_far = COLSCALE ? far : __any_sync(0xffffffffu, far);
         if (!mbar_wait_warp<true>(bar_tfull + 8u * (uint32_t)slot, pass, abort_flag)) { ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem_q + (uint32_t)(slot * SLOT_COLS);
@@ -464,10 +492,28 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             else mbar_arrive(bar_tempty + 8u * (uint32_t)slot);
           }
         };
-        if (!any_far) {
-          const float4* const cs = reinterpret_cast<const float4*>(cw);
-          float r[2][LD];
+        float r[2][LD];
+        tmem_ld_rows(d, r[0]);
+        if (!COLSCALE && any_far) {
+          tmem_wait(r[0]);
+          // a far row's sums are multiplied by the first of two factors where they lie; the others' by one
+          float s1 = 1.0f;
+          if (far) split_factor(a0, w0, s1, s0);
+          __syncwarp();
+#pragma unroll 1
+          for (int c = 0; c < COLS; c += 8) {
+            float v[8];
+            tmem_ld_rows(d + (uint32_t)c, v);
+            tmem_wait(v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], s1);
+            tmem_st_rows(d + (uint32_t)c, v);
+          }
+          tmem_st_wait();
           tmem_ld_rows(d, r[0]);
+        }
+        if (!COLSCALE || !any_far) {
+          const float4* const cs = reinterpret_cast<const float4*>(cw);
           const float2 s = f2(s0);
 #pragma unroll
           for (int c = 0; c < COLS; c += LD) {
@@ -487,7 +533,8 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             }
           }
         } else {
-          // rows and columns without such a factor get the same bits as above
+          // columns without such a factor get the same bits as above
+          tmem_wait(r[0]);
 #pragma unroll
           for (int c = 0; c < COLS; c += 8) {
             float v[8];
@@ -496,9 +543,8 @@ k_fp8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               float& t = i & 1 ? acc[(c + i) / 2].y : acc[(c + i) / 2].x;
-              const float w = COLSCALE ? cw[c + i] : w0;
-              const float near = __fmaf_rn(COLSCALE ? __fmul_rn(v[i], w) : v[i], s0, t);
-              t = choose(COLSCALE ? far_factor(w, w == 0.0f) : far, add_far(t, v[i], a0, w), near);
+              const float w = cw[c + i], near = __fmaf_rn(__fmul_rn(v[i], w), a0, t);
+              t = choose(far_factor(w, w == 0.0f), add_far(t, v[i], a0, w), near);
             }
           }
           give_back();
